@@ -226,6 +226,122 @@ int spcfg_rules_backward(int32_t N, int32_t P, int32_t V, const float* log_root,
                          void* hip_stream);
 
 /*
+ * Layers of the networks that make the rule scores (App. A: symbol embeddings through layers of one matrix product each,
+ * with ReLU and residual, then products with the children's embeddings), and any other dense layer:
+ *   z = x W^T + bias,   y = act(z) + residual
+ *   x dev [rows x in], W dev [out x in], bias dev [out] or NULL, residual dev [rows x out] or NULL, y dev [rows x out]
+ * x, W, bias and the gradients of all three have in_type; y, residual, preact and grad_y have out_type.  All matrices are
+ * row-major and dense; their pointers need no more than the alignment of one element (16-byte alignment of rows is faster).
+ *   in_type F32 (out_type F32): operands are cut exactly into three bf16 pieces and six piece products accumulated in fp32,
+ *     as accurate as an fp32 product.  An infinite operand (or one above 3.38e38, which rounds to an infinite piece) gives NaN.
+ *   in_type BF16 (out_type BF16 or F32): products of the given values accumulated in fp32; the backward pass rounds
+ *     grad_y * act'(z) to bf16, the operands' type.
+ * Activations and epilogues are computed in fp32 and rounded to the result's type once.
+ */
+enum { SPCFG_TYPE_F32 = 0, SPCFG_TYPE_BF16 = 1 };
+enum {
+  SPCFG_ACT_NONE = 0,
+  SPCFG_ACT_RELU = 1, /* max(z, 0); slope 0 at z = 0                    */
+  SPCFG_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2                    */
+  SPCFG_ACT_SILU = 3  /* z / (1 + exp(-z))                              */
+};
+
+/* Plain-old-data description of a layer; set struct_size = sizeof(spcfg_dense_config). */
+typedef struct {
+  uint32_t struct_size;
+  int32_t rows;       /* >= 0; with 0 rows nothing is read, y and grad_x are empty and grad_W, grad_bias are 0     */
+  int32_t in, out;    /* >= 1.  rows, in and out are at most 2^24, rows * in, rows * out and in * out at most 2^36 */
+  int32_t in_type, out_type; /* SPCFG_TYPE_*                                                                       */
+  int32_t activation;        /* SPCFG_ACT_*                                                                        */
+  uint32_t flags;            /* SPCFG_FLAG_ACCUMULATE_GRADS or 0                                                   */
+} spcfg_dense_config;
+
+/* Workspace that either direction of the layer needs (may be 0: workspace may then be NULL). */
+int spcfg_dense_workspace_bytes(const spcfg_dense_config* cfg, size_t* out_bytes);
+
+/*
+ *   preact     dev [rows x out] or NULL: z, for the backward pass (only needed with an activation)
+ *   workspace  dev, 256-byte aligned, >= spcfg_dense_workspace_bytes(...) bytes; holds nothing between calls
+ * residual may be x (where the types and sizes allow it) and y may be residual; outputs overlap nothing else.
+ */
+int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void* W, const void* bias, const void* residual,
+                        void* y, void* preact, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradients of the layer given grad_y; dz = grad_y * act'(z):
+ *   grad_x    dev [rows x in]  dz W + grad_x_add          grad_W    dev [out x in]  dz^T x
+ *   grad_bias dev [out]        sum of dz over the rows
+ * Each may be NULL where it is not wanted (not all three; grad_bias comes with grad_W).  The residual's gradient is grad_y.
+ *   preact      dev [rows x out]: z as the forward call wrote it; NULL with SPCFG_ACT_NONE
+ *   grad_x_add  dev [rows x in] or NULL: added to grad_x.  A layer whose residual is x itself passes grad_y here
+ * SPCFG_FLAG_ACCUMULATE_GRADS adds to grad_W and grad_bias (in their type).  grad_x may be grad_x_add (unless that is
+ * grad_y); outputs overlap nothing else.  Sums run in a fixed order: results are deterministic.
+ */
+int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const void* W, const void* preact, const void* grad_y,
+                         const void* grad_x_add, void* grad_x, void* grad_W, void* grad_bias, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Distillation of rows of scores (emission scores over the vocabulary, rule scores over the children, any logits) from a
+ * teacher's top entries: per row, with p = softmax(teacher / temperature) over the entries that are there and
+ * q = softmax(logits / temperature) over the whole row,
+ *   loss = temperature^2 sum_e p_e (log p_e - log q_id(e)),    lse = log sum_j exp(logits_j / temperature)
+ *   logits         dev [rows x V]            the student's scores, of `type` (SPCFG_TYPE_*)
+ *   teacher_logits dev [rows x k], teacher_ids dev [rows x k] int32: the teacher's kept entries of each row, in any order;
+ *                  an entry with a negative id, or a score of -inf, is absent.  Equal ids add up.  1 <= k <= 1024
+ *   temperature    > 0, finite
+ *   loss, lse      dev [rows] float: out
+ *   grad_loss      dev [rows] float or NULL (= all ones): what each row's loss counts in the sum that is differentiated
+ *   grad_logits    dev [rows x V] of `type`: grad_loss * temperature * (q_j - sum of the p_e with id(e) = j); overwritten,
+ *                  overlaps nothing else
+ *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted)
+ * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An id >= V gives the row's loss and
+ * gradient NaN, and so does a NaN among its scores; a student's score of -inf where p > 0 gives an infinite loss and a
+ * finite gradient.  Matrices are dense, pointers need the alignment of one element.  rows may be 0; rows <= 2^20,
+ * V <= 2^24, rows * V <= 2^36.  Deterministic.
+ */
+int spcfg_distill_workspace_bytes(int32_t rows, int32_t V, size_t* out_bytes);
+int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,
+                          const int32_t* teacher_ids, float temperature, float* loss, float* lse, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+/* The gradient alone, from the lse that a forward call on the same inputs wrote. */
+int spcfg_distill_backward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,
+                           const int32_t* teacher_ids, float temperature, const float* lse, const float* grad_loss,
+                           void* grad_logits, void* hip_stream);
+/* Loss and gradient in one call: every score is read once where a workgroup can hold a row (V <= 16380 floats, 32760 bf16). */
+int spcfg_distill_forward_backward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits,
+                                   const void* teacher_logits, const int32_t* teacher_ids, float temperature,
+                                   const float* grad_loss, float* loss, float* lse, void* grad_logits, void* workspace,
+                                   size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Preference loss on pairs of sentences by their log Z (a sentence and a corrupted copy of it, say), with its gradient in the
+ * form that spcfg_inside_backward takes as grad_logZ:
+ *   margin = (logZ[c] - ref_logZ[c]) - (logZ[r] - ref_logZ[r]),   x = beta * margin
+ *   loss   = (1 - smoothing) log(1 + exp(-x)) + smoothing log(1 + exp(x))
+ *   logZ, ref_logZ   dev [B]: as spcfg_inside writes it; ref_logZ (of a fixed grammar) may be NULL (= 0)
+ *   chosen, rejected dev [pairs] int32: c and r of each pair.  A sentence may be in any number of pairs
+ *   beta > 0, finite; 0 <= smoothing <= 1
+ *   loss, margin     dev [pairs]: out
+ *   grad_loss        dev [pairs] or NULL (= all ones)
+ *   grad_logZ        dev [B]: gradient of sum_p grad_loss[p] * loss[p]; overwritten, 0 for sentences without pairs
+ * A pair with a negative index is absent, and so is one whose margin is a difference of equal infinities (no grammar derives
+ * either sentence): loss, margin and gradient 0.  An index >= B gives loss and margin NaN, and NaN as the gradient of the pair's other
+ * sentence.  Outputs overlap nothing else.  1 <= B <= 65536, 0 <= pairs <= 2^20.  Deterministic; the gradient's cost
+ * grows with B * pairs.
+ */
+int spcfg_preference_forward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,
+                             const int32_t* rejected, float beta, float smoothing, float* loss, float* margin,
+                             void* hip_stream);
+int spcfg_preference_backward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,
+                              const int32_t* rejected, float beta, float smoothing, const float* grad_loss,
+                              float* grad_logZ, void* hip_stream);
+int spcfg_preference_forward_backward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ,
+                                      const int32_t* chosen, const int32_t* rejected, float beta, float smoothing,
+                                      const float* grad_loss, float* loss, float* margin, float* grad_logZ,
+                                      void* hip_stream);
+
+/*
  * Span posteriors (the quantity the reverse pass of the inside algorithm yields, Sec. 3.2: back-propagation
  * through the inside recursion is the outside pass, and beta * d logZ / d beta is the span marginal).
  * Reads the workspace left by spcfg_inside + spcfg_inside_backward (or the fused call) for the same cfg,

@@ -16,6 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libspcfg.so")
 PRECISION_FP32, PRECISION_BF16 = 0, 1
 FLAG_ACCUMULATE_GRADS, FLAG_PER_SENTENCE_GRAMMAR, FLAG_FP32_MFMA, FLAG_BF16_SINGLE_FORWARD = 1, 2, 4, 8
 PROF_CLASSES = 7
+TYPE_F32, TYPE_BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 
 class SpcfgError(RuntimeError):
@@ -27,6 +29,11 @@ class SpcfgError(RuntimeError):
 class Config(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("N", C.c_int32), ("P", C.c_int32), ("max_B", C.c_int32),
                 ("max_n", C.c_int32), ("precision", C.c_int32), ("flags", C.c_uint32)]
+
+
+class DenseConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("in_type", C.c_int32), ("out_type", C.c_int32), ("activation", C.c_int32), ("flags", C.c_uint32)]
 
 
 _lib = None
@@ -55,6 +62,23 @@ def load():
     lib.spcfg_span_marginals.argtypes = [cfgp, vp, i32, i32, vp, sz, vp, vp, vp]
     lib.spcfg_mbr_decode_scratch_bytes.argtypes = [i32, i32, C.POINTER(sz)]
     lib.spcfg_mbr_decode.argtypes = [vp, vp, i32, i32, vp, vp, vp, sz, vp]
+    f32 = C.c_float
+    densep = C.POINTER(DenseConfig)
+    lib.spcfg_dense_workspace_bytes.argtypes = [densep, C.POINTER(sz)]
+    lib.spcfg_dense_forward.argtypes = [densep] + [vp] * 7 + [sz, vp]
+    lib.spcfg_dense_backward.argtypes = [densep] + [vp] * 9 + [sz, vp]
+    lib.spcfg_distill_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+    lib.spcfg_distill_forward.argtypes = [i32] * 4 + [vp, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.spcfg_distill_backward.argtypes = [i32] * 4 + [vp, vp, vp, f32, vp, vp, vp, vp]
+    lib.spcfg_distill_forward_backward.argtypes = [i32] * 4 + [vp, vp, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+    lib.spcfg_preference_forward.argtypes = [i32, i32, vp, vp, vp, vp, f32, f32, vp, vp, vp]
+    lib.spcfg_preference_backward.argtypes = [i32, i32, vp, vp, vp, vp, f32, f32, vp, vp, vp]
+    lib.spcfg_preference_forward_backward.argtypes = [i32, i32, vp, vp, vp, vp, f32, f32, vp, vp, vp, vp, vp]
+    for name in ("spcfg_dense_workspace_bytes", "spcfg_dense_forward", "spcfg_dense_backward",
+                 "spcfg_distill_workspace_bytes", "spcfg_distill_forward", "spcfg_distill_backward",
+                 "spcfg_distill_forward_backward", "spcfg_preference_forward", "spcfg_preference_backward",
+                 "spcfg_preference_forward_backward"):
+        getattr(lib, name).restype = C.c_int
     lib.spcfg_rules_forward.restype = C.c_int
     lib.spcfg_rules_backward.restype = C.c_int
     lib.spcfg_strerror.argtypes = [C.c_int]
@@ -226,6 +250,142 @@ def spcfg_rules_backward(log_root, L, R, emis_logits, emis_lse, tokens, lengths,
         _dev(grad_log_emit, "grad_log_emit", (B, n_max, P)), _dev(grad_root_logits, "grad_root_logits", (N,)),
         _dev(grad_L_logits, "grad_L_logits", (N, M)), _dev(grad_R_logits, "grad_R_logits", (N, M)),
         _dev(grad_emis_logits, "grad_emis_logits", (P, V)), _dev(scratch, "scratch", (32, P)), _stream()))
+
+
+def _here(t, name, shape, type=TYPE_F32, dtype=None):
+    """Pointer of a tensor on torch's current device, of the given element type and shape; None stays None."""
+    import torch
+    if t is None:
+        return None
+    dtype = dtype or (torch.bfloat16 if type == TYPE_BF16 else torch.float32)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
+        raise TypeError(f"{name} must be a contiguous {dtype} device tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device {torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _scratch(workspace):
+    """(pointer, bytes) of a workspace tensor; None where no workspace is needed."""
+    import torch
+    if workspace is None:
+        return None, 0
+    ptr, n = _ws(workspace)
+    if workspace.device.index != torch.cuda.current_device():
+        raise ValueError(f"workspace is on {workspace.device}, not on the current device {torch.cuda.current_device()}")
+    return ptr, n
+
+
+def make_dense_config(rows, n_in, n_out, in_type=TYPE_F32, out_type=TYPE_F32, activation=ACT_NONE, flags=0):
+    return DenseConfig(C.sizeof(DenseConfig), int(rows), int(n_in), int(n_out), int(in_type), int(out_type),
+                       int(activation), int(flags))
+
+
+def spcfg_dense_workspace_bytes(cfg):
+    out = C.c_size_t(0)
+    _check(load().spcfg_dense_workspace_bytes(C.byref(cfg), C.byref(out)))
+    return out.value
+
+
+def spcfg_dense_forward(cfg, x, W, bias, residual, y, preact, workspace):
+    """y = act(x W^T + bias) + residual (see include/spcfg.h); bias, residual and preact may be None."""
+    R, I, O, ti, to = cfg.rows, cfg.n_in, cfg.n_out, cfg.in_type, cfg.out_type
+    wp, wb = _scratch(workspace)
+    _check(load().spcfg_dense_forward(
+        C.byref(cfg), _here(x, "x", (R, I), ti), _here(W, "W", (O, I), ti), _here(bias, "bias", (O,), ti),
+        _here(residual, "residual", (R, O), to), _here(y, "y", (R, O), to), _here(preact, "preact", (R, O), to), wp, wb,
+        _stream()))
+
+
+def spcfg_dense_backward(cfg, x, W, preact, grad_y, grad_x_add, grad_x, grad_W, grad_bias, workspace):
+    """Gradients of spcfg_dense_forward; those that are None are not computed."""
+    R, I, O, ti, to = cfg.rows, cfg.n_in, cfg.n_out, cfg.in_type, cfg.out_type
+    wp, wb = _scratch(workspace)
+    _check(load().spcfg_dense_backward(
+        C.byref(cfg), _here(x, "x", (R, I), ti), _here(W, "W", (O, I), ti), _here(preact, "preact", (R, O), to),
+        _here(grad_y, "grad_y", (R, O), to), _here(grad_x_add, "grad_x_add", (R, I), ti),
+        _here(grad_x, "grad_x", (R, I), ti), _here(grad_W, "grad_W", (O, I), ti),
+        _here(grad_bias, "grad_bias", (O,), ti), wp, wb, _stream()))
+
+
+def _scores_type(logits):
+    import torch
+    types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in types or logits.dim() != 2:
+        raise TypeError("logits must be a two-dimensional float32 or bfloat16 device tensor")
+    return types[logits.dtype]
+
+
+def spcfg_distill_workspace_bytes(rows, V):
+    out = C.c_size_t(0)
+    _check(load().spcfg_distill_workspace_bytes(int(rows), int(V), C.byref(out)))
+    return out.value
+
+
+def _distill_inputs(logits, teacher_logits, teacher_ids, temperature):
+    import torch
+    type = _scores_type(logits)
+    (rows, V), k = logits.shape, teacher_ids.shape[-1]
+    return type, rows, V, k, [
+        type, rows, V, k, _here(logits, "logits", (rows, V), type), _here(teacher_logits, "teacher_logits", (rows, k), type),
+        _here(teacher_ids, "teacher_ids", (rows, k), dtype=torch.int32), float(temperature)]
+
+
+def spcfg_distill_forward(logits, teacher_logits, teacher_ids, temperature, loss, lse, workspace):
+    """Loss of every row of logits [rows, V] against a teacher's top entries [rows, k], and the rows' logsumexp."""
+    _, rows, _, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    wp, wb = _scratch(workspace)
+    _check(load().spcfg_distill_forward(*inputs, _here(loss, "loss", (rows,)), _here(lse, "lse", (rows,)), wp, wb, _stream()))
+
+
+def spcfg_distill_backward(logits, teacher_logits, teacher_ids, temperature, lse, grad_loss, grad_logits):
+    """Gradient of spcfg_distill_forward's losses, from the lse that it wrote."""
+    type, rows, V, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    _check(load().spcfg_distill_backward(
+        *inputs, _here(lse, "lse", (rows,)), _here(grad_loss, "grad_loss", (rows,)),
+        _here(grad_logits, "grad_logits", (rows, V), type), _stream()))
+
+
+def spcfg_distill_forward_backward(logits, teacher_logits, teacher_ids, temperature, grad_loss, loss, lse, grad_logits,
+                                   workspace):
+    """Loss and gradient in one call."""
+    type, rows, V, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    wp, wb = _scratch(workspace)
+    _check(load().spcfg_distill_forward_backward(
+        *inputs, _here(grad_loss, "grad_loss", (rows,)), _here(loss, "loss", (rows,)), _here(lse, "lse", (rows,)),
+        _here(grad_logits, "grad_logits", (rows, V), type), wp, wb, _stream()))
+
+
+def _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing):
+    import torch
+    (B,), (n,) = logZ.shape, chosen.shape
+    return B, n, [B, n, _here(logZ, "logZ", (B,)), _here(ref_logZ, "ref_logZ", (B,)),
+                  _here(chosen, "chosen", (n,), dtype=torch.int32), _here(rejected, "rejected", (n,), dtype=torch.int32),
+                  float(beta), float(smoothing)]
+
+
+def spcfg_preference_forward(logZ, ref_logZ, chosen, rejected, beta, smoothing, loss, margin):
+    """Loss and margin of every pair of sentences (see include/spcfg.h); ref_logZ may be None."""
+    _, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    _check(load().spcfg_preference_forward(*inputs, _here(loss, "loss", (n,)), _here(margin, "margin", (n,)), _stream()))
+
+
+def spcfg_preference_backward(logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, grad_logZ):
+    """Gradient of the pairs' losses in logZ, as spcfg_inside_backward takes it."""
+    B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    _check(load().spcfg_preference_backward(*inputs, _here(grad_loss, "grad_loss", (n,)),
+                                            _here(grad_logZ, "grad_logZ", (B,)), _stream()))
+
+
+def spcfg_preference_forward_backward(logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, loss, margin,
+                                      grad_logZ):
+    """Loss, margin and gradient in one call."""
+    B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    _check(load().spcfg_preference_forward_backward(
+        *inputs, _here(grad_loss, "grad_loss", (n,)), _here(loss, "loss", (n,)), _here(margin, "margin", (n,)),
+        _here(grad_logZ, "grad_logZ", (B,)), _stream()))
 
 
 def spcfg_span_marginals(cfg, lengths, n_max, workspace, span_post, span_label=None):

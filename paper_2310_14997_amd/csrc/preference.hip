@@ -1,0 +1,139 @@
+// Preference loss on pairs of sentences, by their log Z (a sentence and a corrupted copy, or any better and worse one), and
+// its gradient, in the form that the reverse pass of the inside algorithm takes:
+//   margin = (logZ_c - ref_c) - (logZ_r - ref_r),   x = beta margin
+//   loss   = (1 - eps) softplus(-x) + eps softplus(x)
+//   d loss / d margin = beta (eps s(x) - (1 - eps) s(-x)),  s(x) = 1 / (1 + exp(-x)); + at c, - at r
+// One launch: workgroups of the first kind take the pairs, those of the second kind sentences, a wavefront for each four:
+// it looks through all pairs, 64 at a time, and adds the ones that its sentences are part of.  No atomics: a sentence
+// in many pairs has its sum in a fixed order (lane by lane, then across lanes), in 64 bits, as are the differences of log
+// Z, which are small beside log Z itself.  Bound by latency at the sizes of a batch.
+#include <cmath>
+
+#include "spcfg_internal.h"
+
+namespace spcfg {
+namespace {
+
+constexpr int kOwn = 4;        // sentences of a wavefront
+constexpr int kMostPairs = 1 << 20, kMostSentences = 1 << 16;
+
+struct Args {
+  int B, n;
+  const float *logZ, *ref;
+  const int32_t *chosen, *rejected;
+  float beta, eps;
+  const float* grad_loss;
+  float *loss, *margin, *grad;
+};
+
+// margin of pair (i, j): out of range NaN; both sides infinite alike (two sentences that cannot be derived) 0 with *out set, as
+// for an absent pair
+__device__ __forceinline__ float margin_of(const Args& g, int i, int j, bool* out) {
+  *out = i < 0 || j < 0;
+  if (*out) return 0.0f;
+  if (i >= g.B || j >= g.B) return NAN;
+  const float a = g.logZ[i], b = g.logZ[j];
+  const float ra = g.ref ? g.ref[i] : 0.0f, rb = g.ref ? g.ref[j] : 0.0f;
+  const double d = ((double)a - ra) - ((double)b - rb);
+  if (d != d && a == a && b == b && ra == ra && rb == rb) {
+    *out = true;
+    return 0.0f;
+  }
+  return (float)d;
+}
+
+__device__ __forceinline__ float weight_of(const Args& g, float margin) {
+  const float x = g.beta * margin;
+  return g.beta * (g.eps / (1.0f + expf(-x)) - (1.0f - g.eps) / (1.0f + expf(x)));
+}
+
+__global__ void __launch_bounds__(256) k_preference(Args g, int pair_blocks) {
+  if ((int)blockIdx.x < pair_blocks) {
+    const int p = blockIdx.x * 256 + threadIdx.x;
+    if (p >= g.n) return;
+    bool out;
+    const float m = margin_of(g, g.chosen[p], g.rejected[p], &out);
+    const float x = g.beta * m, tail = log1pf(expf(-fabsf(x)));
+    // (an infinite margin times a smoothing of 0 would be NaN)
+    const float lo = fmaxf(-x, 0.0f) + tail, hi = fmaxf(x, 0.0f) + tail;
+    const float l = (g.eps < 1.0f ? (1.0f - g.eps) * lo : 0.0f) + (g.eps > 0.0f ? g.eps * hi : 0.0f);
+    g.loss[p] = out ? 0.0f : m != m ? m : l;
+    g.margin[p] = m;
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  const int s0 = (((int)blockIdx.x - pair_blocks) * 4 + (int)(threadIdx.x >> 6)) * kOwn;
+  if (s0 >= g.B) return;
+  double acc[kOwn] = {};
+  for (int p = lane; p < g.n; p += 64) {
+    const int i = g.chosen[p], j = g.rejected[p];
+    if ((i < s0 || i >= s0 + kOwn) && (j < s0 || j >= s0 + kOwn)) continue;
+    bool out;
+    const float m = margin_of(g, i, j, &out);
+    if (out || i == j) continue;  // (a sentence against itself adds and takes away the same)
+    const double w = (double)weight_of(g, m) * (g.grad_loss ? g.grad_loss[p] : 1.0f);
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u) {
+      if (i == s0 + u) acc[u] += w;
+      if (j == s0 + u) acc[u] -= w;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kOwn; ++u) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc[u] += __shfl_xor(acc[u], o, 64);
+    if (lane == 0 && s0 + u < g.B) g.grad[s0 + u] = (float)acc[u];
+  }
+}
+
+int run(int32_t B, int32_t n, const float* logZ, const float* ref, const int32_t* chosen, const int32_t* rejected, float beta,
+        float eps, const float* grad_loss, float* loss, float* margin, float* grad, bool forward, bool backward, hipStream_t st) {
+  if (B < 1 || B > kMostSentences || n < 0 || n > kMostPairs) return SPCFG_ERR_SHAPE;
+  if (!(beta > 0.0f) || !(beta < INFINITY) || !(eps >= 0.0f) || !(eps <= 1.0f)) return SPCFG_ERR_ARG;
+  if (!logZ || (n > 0 && (!chosen || !rejected)) || (n > 0 && forward && (!loss || !margin)) || (backward && !grad)) return SPCFG_ERR_ARG;
+  // outputs are written while other workgroups read the inputs: none may share memory with anything else
+  const struct { const void* p; int64_t len; } at[] = {
+      {forward ? loss : nullptr, n}, {forward ? margin : nullptr, n}, {backward ? grad : nullptr, B},
+      {logZ, B}, {ref, B}, {chosen, n}, {rejected, n}, {grad_loss, n}};
+  for (int o = 0; o < 3; ++o)
+    for (int i = 0; i < 8; ++i) {
+      const uintptr_t a = (uintptr_t)at[o].p, b = (uintptr_t)at[i].p;
+      if (o != i && a && b && a < b + 4 * at[i].len && b < a + 4 * at[o].len) return SPCFG_ERR_ARG;
+    }
+  const int pb = forward ? (n + 255) / 256 : 0, sb = backward ? (B + 4 * kOwn - 1) / (4 * kOwn) : 0;
+  if (pb + sb == 0) return SPCFG_OK;
+  const Args a{B, n, logZ, ref, chosen, rejected, beta, eps, grad_loss, loss, margin, grad};
+  hipLaunchKernelGGL(k_preference, dim3(pb + sb), dim3(256), 0, st, a, pb);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace spcfg
+
+using namespace spcfg;
+
+extern "C" {
+
+int spcfg_preference_forward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,
+                             const int32_t* rejected, float beta, float smoothing, float* loss, float* margin,
+                             void* hip_stream) {
+  return run(B, pairs, logZ, ref_logZ, chosen, rejected, beta, smoothing, nullptr, loss, margin, nullptr, true, false,
+             (hipStream_t)hip_stream);
+}
+
+int spcfg_preference_backward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,
+                              const int32_t* rejected, float beta, float smoothing, const float* grad_loss,
+                              float* grad_logZ, void* hip_stream) {
+  return run(B, pairs, logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, nullptr, nullptr, grad_logZ, false, true,
+             (hipStream_t)hip_stream);
+}
+
+int spcfg_preference_forward_backward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ,
+                                      const int32_t* chosen, const int32_t* rejected, float beta, float smoothing,
+                                      const float* grad_loss, float* loss, float* margin, float* grad_logZ,
+                                      void* hip_stream) {
+  return run(B, pairs, logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, loss, margin, grad_logZ, true, true,
+             (hipStream_t)hip_stream);
+}
+
+}  // extern "C"

@@ -349,6 +349,12 @@ int hip_status() {
   return SPCFG_ERR_HIP;
 }
 
+}  // namespace
+
+int launch_status() { return hip_status(); }
+
+namespace {
+
 int check_ws(const Layout& ly, void* ws, size_t bytes) {
   if (!ws) return SPCFG_ERR_ARG;
   if (((uintptr_t)ws & 255) != 0 || bytes < ly.total) return SPCFG_ERR_WORKSPACE;

@@ -42,6 +42,9 @@ namespace spcfg {
 
 constexpr int kPad = 64;                 // N and P are padded to multiples of this (zero filled)
 constexpr int kExpZero = -(1 << 24);     // exponent marking an all-zero vector
+// Status of the launches of a call, for every entry point outside spcfg_api.hip too: keeps the runtime's message.
+int launch_status();
+
 constexpr int kMaxB = 960;               // lengths travel as one kernel argument
 constexpr int kMaxLen = 1024;
 
