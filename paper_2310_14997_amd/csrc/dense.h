@@ -53,8 +53,45 @@ struct Args {
   void *y, *preact, *grad_x, *grad_W, *grad_bias;
 };
 
+// The three products of a layer: z = x W^T, dx = dz W, dW = dz^T x.
+enum { FWD = 0, DX = 1, DW = 2 };
+
+// Epilogue of one element (m, n) of a product, whose sum is s.
+template <typename TI, typename TO, int FORM>
+__device__ __forceinline__ void store_one(const Args& g, int64_t m, int64_t n, float s) {
+  const int64_t at = m * (FORM == FWD ? g.O : g.I) + n;
+  if constexpr (FORM == FWD) {
+    if (g.bias) s += to_float<TI>(static_cast<const TI*>(g.bias)[n]);
+    if (g.preact) static_cast<TO*>(g.preact)[at] = from_float<TO>(s);
+    s = act_value(g.act, s);
+    if (g.residual) s += to_float<TO>(static_cast<const TO*>(g.residual)[at]);
+    static_cast<TO*>(g.y)[at] = from_float<TO>(s);
+  } else if constexpr (FORM == DX) {
+    if (g.grad_x_add) s += to_float<TI>(static_cast<const TI*>(g.grad_x_add)[at]);
+    static_cast<TI*>(g.grad_x)[at] = from_float<TI>(s);
+  } else {
+    TI* o = static_cast<TI*>(g.grad_W) + at;
+    if (g.accumulate) s += to_float<TI>(*o);
+    *o = from_float<TI>(s);
+  }
+}
+template <typename TI>
+__device__ __forceinline__ void store_bias(const Args& g, int64_t m, float s) {
+  TI* o = static_cast<TI*>(g.grad_bias) + m;
+  if (g.accumulate) s += to_float<TI>(*o);
+  *o = from_float<TI>(s);
+}
+
+inline bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
 void launch_direct_forward(const Args& a, int in_type, int out_type, hipStream_t st);
 void launch_direct_backward(const Args& a, int in_type, int out_type, hipStream_t st);
+
+// Tiled products (dense_tile.hip): workspace of a layer, 0 where none of its products takes them
+size_t tiled_workspace(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act);
+// whether these take the call: sizes, and alignment of what is read as it lies
+bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
+bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
 
 }  // namespace dense
 }  // namespace spcfg

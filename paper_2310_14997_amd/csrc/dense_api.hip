@@ -20,7 +20,9 @@ int check(const spcfg_dense_config* c) {
   return SPCFG_OK;
 }
 
-size_t need(const spcfg_dense_config*) { return 0; }
+size_t need(const spcfg_dense_config* c) {
+  return c->rows == 0 ? 0 : dense::tiled_workspace(c->rows, c->in, c->out, c->in_type, c->out_type, c->activation);
+}
 
 int check_workspace(const spcfg_dense_config* c, const void* ws, size_t bytes) {
   const size_t n = need(c);
@@ -80,7 +82,8 @@ int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void
   if (overlap(y, ny, to, preact, ny, to)) return SPCFG_ERR_ARG;
   if ((rc = check_workspace(cfg, workspace, workspace_bytes))) return rc;
   a.x = x; a.W = W; a.bias = bias; a.residual = residual; a.y = y; a.preact = preact;
-  dense::launch_direct_forward(a, ti, to, (hipStream_t)hip_stream);
+  if (!dense::tiled_forward(a, ti, to, workspace, (hipStream_t)hip_stream))
+    dense::launch_direct_forward(a, ti, to, (hipStream_t)hip_stream);
   return launch_status();
 }
 
@@ -113,7 +116,8 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
   if (cfg->rows == 0 && !grad_W) return SPCFG_OK;
   a.x = x; a.W = W; a.preact_in = act ? preact : nullptr; a.grad_y = grad_y; a.grad_x_add = grad_x_add;
   a.grad_x = cfg->rows > 0 ? grad_x : nullptr; a.grad_W = grad_W; a.grad_bias = grad_bias;
-  dense::launch_direct_backward(a, ti, to, (hipStream_t)hip_stream);
+  if (cfg->rows == 0 || !dense::tiled_backward(a, ti, to, workspace, (hipStream_t)hip_stream))
+    dense::launch_direct_backward(a, ti, to, (hipStream_t)hip_stream);
   return launch_status();
 }
 

@@ -17,7 +17,6 @@ namespace dense {
 namespace {
 
 constexpr int kWaves = 8;
-enum { FWD = 0, DX = 1, DW = 2 };
 
 // pieces of eight K values of one row, ready for the matrix instruction
 template <typename T> struct Pieces;
@@ -183,21 +182,7 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += lds[w * kTile + e];
-    const int64_t at = m * N + n;
-    if constexpr (FORM == FWD) {
-      if (g.bias) s += to_float<TI>(static_cast<const TI*>(g.bias)[n]);
-      if (g.preact) static_cast<TO*>(g.preact)[at] = from_float<TO>(s);
-      s = act_value(g.act, s);
-      if (g.residual) s += to_float<TO>(static_cast<const TO*>(g.residual)[at]);
-      static_cast<TO*>(g.y)[at] = from_float<TO>(s);
-    } else if constexpr (FORM == DX) {
-      if (g.grad_x_add) s += to_float<TI>(static_cast<const TI*>(g.grad_x_add)[at]);
-      static_cast<TI*>(g.grad_x)[at] = from_float<TI>(s);
-    } else {
-      TI* o = static_cast<TI*>(g.grad_W) + at;
-      if (g.accumulate) s += to_float<TI>(*o);
-      *o = from_float<TI>(s);
-    }
+    store_one<TI, TO, FORM>(g, m, n, s);
   }
   if (FORM == DW && g.grad_bias && tn == 0 && threadIdx.x < 32 * MT) {
     const int64_t m = m0 + threadIdx.x;
@@ -206,9 +191,7 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
       float s = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) s += bl[(w * MT + i) * 64 + l] + bl[(w * MT + i) * 64 + 32 + l];
-      TI* o = static_cast<TI*>(g.grad_bias) + m;
-      if (g.accumulate) s += to_float<TI>(*o);
-      *o = from_float<TI>(s);
+      store_bias<TI>(g, m, s);
     }
   }
 }
@@ -230,7 +213,6 @@ __global__ void __launch_bounds__(64 * kWaves) k_dense_backward(Args g, unsigned
   else tile_product<TI, TO, DW, VEC, MT, NT>(g, (b - tiles_x) / tiles_i, (b - tiles_x) % tiles_i, lds);
 }
 
-bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
 
 template <typename TI, typename TO>

@@ -1,0 +1,602 @@
+// Dense layers, large products: C[m][n] = sum_k A(m,k) B(n,k) on tiles in LDS, operands as bf16 planes.
+//
+//  * bf16 operands are one plane, read where they lie; fp32 operands are cut exactly into three (nt::Split3: hi, mid, lo) by
+//    k_dense_cut and multiplied as six piece products, accumulated in fp32; dz = grad_y * act'(z) is written as one or
+//    three planes by k_dense_dz, which adds up the bias's gradient on the way (not needed where grad_y is bf16 and there is
+//    no activation: dz is grad_y).
+//  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
+//    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
+//    32 values of k: rows of 64 bytes along k, with the 16-byte piece XORed with bits 2..3 of the row; across k 32 rows of
+//    128 columns, with the 64-byte piece XORed with the row mod 4.  Operands come out of LDS with ds_read_b128, resp. with the
+//    transposing ds_read_b64_tr_b16; both forms meet no bank conflict.
+//  * The order of a step is written out: products of the step's first 16 k while its second 16 are read, then products of
+//    those; behind their first the barrier - each wavefront's loads of the next step have landed, nobody needs this step's
+//    tiles any more - then the next step's first operands are read and its place is filled with the tiles of step + NS.
+//  * Few tiles: k is split over workgroups, which leave fp32 partial tiles; k_dense_join adds them in order.
+// No launch waits for another workgroup; sums run in an order fixed by the sizes.
+#include <type_traits>
+#include <utility>
+
+#include "dense.h"
+
+namespace spcfg {
+namespace dense {
+
+namespace {
+
+using nt::dma16;
+using nt::lds_address;
+using nt::static_for;
+
+typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
+
+constexpr int BK = 32;  // values of k of a step
+
+// What lies beyond the end of k reads as zero.
+__device__ uintx4 g_zeros;
+
+struct Product {
+  const uint16_t *A, *B;
+  int64_t lda, ldb, plane_a, plane_b;  // in elements
+  int64_t M, N, K;                     // K: rows, resp. columns that may be read along k
+  int steps, steps_per_split, splits;
+  unsigned tiles_m, tiles_n;
+  float* partial;                      // [splits][M][N] where splits > 1
+  const float* bias_part;              // dW: [bias_parts][O] sums of dz over parts of the rows
+  int bias_parts, bias_blocks;
+};
+
+// One operand of one plane: eight k of a row or column per lane.
+struct Frag { uintx2 lo, hi; };
+__device__ __forceinline__ bf16x8 operand(const Frag& f) {
+  return __builtin_bit_cast(bf16x8, uintx4{f.lo[0], f.lo[1], f.hi[0], f.hi[1]});
+}
+__device__ __forceinline__ bf16x8 operand(const uintx4& f) { return __builtin_bit_cast(bf16x8, f); }
+__device__ __forceinline__ void tie(Frag& f) { asm volatile("" : "+v"(f.lo), "+v"(f.hi)); }
+__device__ __forceinline__ void tie(uintx4& f) { asm volatile("" : "+v"(f)); }
+
+// PL planes; a tile of BM x BN by WM x WN wavefronts; NS steps in LDS; TA / TB: the operand runs across k
+template <int PL_, int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
+  static constexpr int PL = PL_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
+  static constexpr int NW = WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN);
+  static constexpr int PTA = BM * 64, PTB = BN * 64;  // bytes of one plane's tile
+  static constexpr int STAGE = PL * (PTA + PTB);
+  static constexpr int ND = PL * (BM + BN) / 16 / NW;  // 1 KB loads of a wavefront and step
+  static constexpr int NM = (PL == 3 ? 6 : 1) * MI * NI;
+  static constexpr int kLds = NS * STAGE;
+  static constexpr int NDA = PL * BM / 16 / NW;          // the first of them of A
+  static_assert((BM / 16) % NW == 0 && (BN / 16) % NW == 0, "loads of a plane's tile are dealt evenly");
+};
+
+#define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
+
+template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
+__global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW / 4 : S::NW / 4) k_dense_tile(Args g, Product p) {
+  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS;
+  __shared__ __align__(1024) unsigned char lds[S::kLds];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % S::WM, wn = wave / S::WM;
+
+  if (FORM == DW && (int)blockIdx.x < p.bias_blocks) {
+    // the bias's gradient: 64 columns a workgroup, the parts dealt to the wavefronts, joined in their order
+    float* red = reinterpret_cast<float*>(lds);
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < p.M) {
+#pragma unroll 4
+      for (int q = wave; q < p.bias_parts; q += S::NW) s += p.bias_part[(int64_t)q * p.M + c];
+    }
+    red[wave * 64 + lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < p.M) {
+#pragma unroll
+      for (int w = 1; w < S::NW; ++w) s += red[w * 64 + lane];
+      store_bias<TI>(g, c, s);
+    }
+    return;
+  }
+
+  // which tile: each XCD takes a run of consecutive ones, which form blocks of up to 8 row tiles
+  unsigned t;
+  {
+    const unsigned b = blockIdx.x - (FORM == DW ? p.bias_blocks : 0), n = gridDim.x - (FORM == DW ? p.bias_blocks : 0);
+    const unsigned xcd = b & 7, q = n >> 3, r = n & 7;
+    t = xcd * q + min(xcd, r) + (b >> 3);
+  }
+  const unsigned per_split = p.tiles_m * p.tiles_n;
+  const int split = t / per_split;
+  t -= split * per_split;
+  const unsigned band = t / (8 * p.tiles_n), rows_here = min(8u, p.tiles_m - band * 8), in_band = t - band * 8 * p.tiles_n;
+  const int64_t m0 = (int64_t)(band * 8 + in_band % rows_here) * S::BM, n0 = (int64_t)(in_band / rows_here) * S::BN;
+  const int k0 = split * p.steps_per_split, k1 = min(p.steps, k0 + p.steps_per_split);
+
+  // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 bytes; across: 4 of 256.
+  const unsigned lds0 = lds_address(lds);
+  const unsigned char* gp[ND];
+  unsigned e_lds[ND];
+  const int r_al = lane >> 2, c_al = (lane & 3) ^ ((lane >> 4) & 3);  // row of the 16, and piece: XOR with bits 2..3 of the row
+  const int r_ac = lane >> 4, c_ac = (((lane & 15) >> 2) ^ r_ac) * 32 + (lane & 3) * 8;
+  const int64_t step_a = TA ? 2 * BK * p.lda : 2 * BK, step_b = TB ? 2 * BK * p.ldb : 2 * BK;  // bytes a step
+  static_for<0, ND>([&](auto j) {
+    constexpr int jv = decltype(j)::value;
+    constexpr bool isA = jv < S::NDA;
+    constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
+    const int q = wave + e0 % per;
+    e_lds[jv] = (unsigned)((isA ? plane * S::PTA : PL * S::PTA + plane * S::PTB) + q * 1024);
+    const uint16_t* base = isA ? p.A + plane * p.plane_a : p.B + plane * p.plane_b;
+    const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
+    if (isA ? TA : TB) {
+      const int64_t col = min(o0 + (q >> 3) * 128 + c_ac, (len + 7) / 8 * 8 - 8);
+      gp[jv] = reinterpret_cast<const unsigned char*>(base + (4 * (q & 7) + r_ac) * ld + col);
+    } else {
+      gp[jv] = reinterpret_cast<const unsigned char*>(base + min(o0 + 16 * q + r_al, len - 1) * ld + c_al * 8);
+    }
+  });
+  auto load_one = [&](auto j, unsigned stage, int kt) {
+    constexpr int jv = decltype(j)::value;
+    constexpr bool isA = jv < S::NDA;
+    constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA);
+    const int64_t k = (int64_t)kt * BK + ((isA ? TA : TB) ? 4 * ((wave + e0 % per) & 7) + r_ac : c_al * 8);
+    const unsigned char* at = gp[jv] + kt * (isA ? step_a : step_b);
+    dma16(k < p.K ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
+  };
+
+  // operand reads: byte offsets inside a stage of the fragments of the first 16 k of plane 0
+  unsigned fa[TA ? MI : 1], fb[TB ? NI : 1];
+  {
+    const int fr = lane & 31, fh = lane >> 5;
+    const unsigned al = (unsigned)(fr * 64 + (fh ^ ((fr >> 2) & 3)) * 16);
+    const int li = lane & 15, lq = lane >> 4;
+    const unsigned ac = (unsigned)((8 * (lq >> 1) + (li >> 2)) * 256 + 32 * (lq & 1) + 8 * (li & 3));
+    if constexpr (TA) {
+#pragma unroll
+      for (int f = 0; f < MI; ++f) {
+        const int blk = wm * MI + f;
+        fa[f] = ac + (unsigned)((blk >> 2) * 8192 + (((blk & 3) ^ (li >> 2)) * 64));
+      }
+    } else {
+      fa[0] = al + (unsigned)(wm * MI * 2048);
+    }
+    if constexpr (TB) {
+#pragma unroll
+      for (int f = 0; f < NI; ++f) {
+        const int blk = wn * NI + f;
+        fb[f] = PL * S::PTA + ac + (unsigned)((blk >> 2) * 8192 + (((blk & 3) ^ (li >> 2)) * 64));
+      }
+    } else {
+      fb[0] = PL * S::PTA + al + (unsigned)(wn * NI * 2048);
+    }
+  }
+  using FA = typename std::conditional<TA, Frag, uintx4>::type;
+  using FB = typename std::conditional<TB, Frag, uintx4>::type;
+  struct Chunk { FA a[PL][MI]; FB b[PL][NI]; };
+  Chunk X, Y;
+  // fragment r of a chunk: planes of A, then of B
+  constexpr int NF = PL * (MI + NI);
+  auto read_one = [&](Chunk& F, auto r, unsigned stage, auto chunk) {
+    constexpr int rv = decltype(r)::value, cv = decltype(chunk)::value;
+    if constexpr (rv < PL * MI) {
+      constexpr int pl = rv / MI, f = rv % MI;
+      if constexpr (TA) {
+        const unsigned at = lds0 + stage + fa[f];
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].lo) : "v"(at), "n"(pl * S::PTA + cv * 4096));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 4096 + 1024));
+      } else {
+        const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"(pl * S::PTA + f * 2048));
+      }
+    } else {
+      constexpr int pl = (rv - PL * MI) / NI, f = (rv - PL * MI) % NI;
+      if constexpr (TB) {
+        const unsigned at = lds0 + stage + fb[f];
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].lo) : "v"(at), "n"(pl * S::PTB + cv * 4096));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 4096 + 1024));
+      } else {
+        const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"(pl * S::PTB + f * 2048));
+      }
+    }
+  };
+  auto wait_reads = [&](Chunk& F) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int pl = 0; pl < PL; ++pl) {
+#pragma unroll
+      for (int f = 0; f < MI; ++f) tie(F.a[pl][f]);
+#pragma unroll
+      for (int f = 0; f < NI; ++f) tie(F.b[pl][f]);
+    }
+  };
+  floatx16 acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+  auto mfma_one = [&](Chunk& F, auto i) {
+    // three planes: lo*hi, hi*lo, mid*mid, mid*hi, hi*mid, hi*hi (0 hi, 1 mid, 2 lo)
+    constexpr int pp = decltype(i)::value / (MI * NI), rem = decltype(i)::value % (MI * NI), mi = rem / NI, ni = rem % NI;
+    constexpr int pa = PL == 1 ? 0 : pp == 0 ? 2 : (pp == 2 || pp == 3 ? 1 : 0);
+    constexpr int pb = PL == 1 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
+    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(F.a[pa][mi]), operand(F.b[pb][ni]), acc[mi][ni], 0, 0, 0);
+  };
+  using C0 = std::integral_constant<int, 0>;
+  using C1 = std::integral_constant<int, 1>;
+
+  const int n = k1 - k0;
+  static_for<0, NS>([&](auto s) {
+    constexpr int sv = decltype(s)::value;
+    if (sv < n) static_for<0, ND>([&](auto j) { load_one(j, sv * S::STAGE, k0 + sv); });
+  });
+  if (n >= NS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND * (NS - 1)) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  SPCFG_SB
+  if (n > 0) static_for<0, NF>([&](auto r) { read_one(X, r, 0u, C0{}); });
+  unsigned cur = 0;
+  constexpr int RPF = (NF + NM - 1) / NM;                          // reads behind each product of the first half
+  constexpr int NB = NM >= 8 ? 2 : 1, RS = NM - NB;                // products ahead of the barrier, and behind it
+  constexpr int RPS = RS > 0 ? (NF + RS - 1) / RS : NF;
+  for (int i = 0; i < n; ++i) {
+    const unsigned nxt = cur + S::STAGE == NS * S::STAGE ? 0 : cur + S::STAGE;
+    SPCFG_SB
+    wait_reads(X);
+    SPCFG_SB
+    static_for<0, NM>([&](auto m) {
+      constexpr int mv = decltype(m)::value;
+      mfma_one(X, m);
+      SPCFG_SB
+      static_for<0, RPF>([&](auto q) {
+        constexpr int r = mv * RPF + decltype(q)::value;
+        if constexpr (r < NF) read_one(Y, std::integral_constant<int, r>{}, cur, C1{});
+      });
+      SPCFG_SB
+    });
+    wait_reads(Y);
+    SPCFG_SB
+    static_for<0, NB>([&](auto m) { mfma_one(Y, m); });
+    SPCFG_SB
+    if (i + NS <= n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND * (NS - 2)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    SPCFG_SB
+    const bool more = i + NS < n;
+    static_for<NB, NM>([&](auto m) {
+      constexpr int s = decltype(m)::value - NB;
+      mfma_one(Y, m);
+      SPCFG_SB
+      static_for<0, RPS>([&](auto q) {
+        constexpr int r = s * RPS + decltype(q)::value;
+        if constexpr (r < NF) read_one(X, std::integral_constant<int, r>{}, nxt, C0{});
+      });
+      if (more) {
+        static_for<0, ND>([&](auto j) {
+          if constexpr ((decltype(j)::value * RS) / ND == s) load_one(j, cur, k0 + i + NS);
+        });
+      }
+      SPCFG_SB
+    });
+    cur = nxt;
+  }
+  wait_reads(X);  // (the last step read ahead into a place without new data: nothing of it is used)
+
+  // accumulators of a 32 x 32 tile: column lane % 32, row 8 (v / 4) + 4 (lane / 32) + v % 4
+  const int64_t mw = m0 + wm * MI * 32 + 4 * (lane >> 5), nw = n0 + wn * NI * 32 + (lane & 31);
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int64_t m = mw + mi * 32 + 8 * (v >> 2) + (v & 3);
+      if (m >= p.M) continue;
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) {
+        const int64_t c = nw + ni * 32;
+        if (c >= p.N) continue;
+        if (p.splits > 1) p.partial[((int64_t)split * p.M + m) * p.N + c] = acc[mi][ni][v];
+        else store_one<TI, TO, FORM>(g, m, c, acc[mi][ni][v]);
+      }
+    }
+}
+
+template <typename TI, typename TO, int FORM>
+__global__ void __launch_bounds__(256) k_dense_join(Args g, Product p) {
+  const int64_t n = p.M * p.N;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
+    float s = p.partial[e];
+    for (int q = 1; q < p.splits; ++q) s += p.partial[(int64_t)q * n + e];
+    store_one<TI, TO, FORM>(g, e / p.N, e % p.N, s);
+  }
+}
+
+// ---- planes --------------------------------------------------------------------------------------------------------------
+// Rows and columns of a matrix in planes are rounded up to a step's 32, with zeros, so that products may run along either.
+int64_t up32(int64_t n) { return (n + 31) / 32 * 32; }
+
+struct Cut {
+  const void* src[2];
+  uint16_t* dst[2];
+  int64_t rows[2], cols[2];
+  unsigned blocks0;  // workgroups of the first matrix
+};
+
+__device__ __forceinline__ void put_planes(uint16_t* dst, int64_t plane, const float (&v)[8], float) {
+  Split3 s;
+  s.cut(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]));
+  *reinterpret_cast<uintx4*>(dst) = s.hi;
+  *reinterpret_cast<uintx4*>(dst + plane) = s.mid;
+  *reinterpret_cast<uintx4*>(dst + 2 * plane) = s.lo;
+}
+__device__ __forceinline__ void put_planes(uint16_t* dst, int64_t, const float (&v)[8], uint16_t) {
+  uintx4 h;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = Split3::pack_rne(v[2 * i], v[2 * i + 1]);
+  *reinterpret_cast<uintx4*>(dst) = h;
+}
+
+// eight values of a row from column c on, zero outside the matrix
+template <typename T>
+__device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, bool vec, float (&v)[8]) {
+  T x[8];
+  if (vec && r < rows && c + 8 <= cols) {
+    uintx4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uintx4*>(src + r * cols + c)[i];
+    __builtin_memcpy(x, w, sizeof(x));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = r < rows && c + i < cols ? src[r * cols + c + i] : T(0);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_float<T>(x[i]);
+}
+
+// The planes of one or two matrices.  Bound by HBM: fp32 10 bytes a value.
+template <typename T>
+__global__ void __launch_bounds__(256) k_dense_cut(Cut c) {
+  const int w = blockIdx.x >= c.blocks0;
+  const T* src = static_cast<const T*>(c.src[w]);
+  const int64_t rows = c.rows[w], cols = c.cols[w], ld = (cols + 31) / 32 * 32, rows32 = (rows + 31) / 32 * 32;
+  const int64_t e = ((int64_t)(blockIdx.x - (w ? c.blocks0 : 0)) * 256 + threadIdx.x) * 8;
+  if (e >= rows32 * ld) return;
+  const int64_t r = e / ld, col = e % ld;
+  const bool vec = ((((uintptr_t)src) | (uintptr_t)(cols * sizeof(T))) & 15) == 0;
+  float v[8];
+  eight<T>(src, rows, cols, r, col, vec, v);
+  put_planes(c.dst[w] + e, rows32 * ld, v, T());
+}
+
+// dz = grad_y * act'(z) in planes (where dst is given) and, part by part of the rows, its sums over them (where sums is): 512
+// columns and `span` rows a workgroup, a row per wavefront at a time.
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) k_dense_dz(Args g, uint16_t* __restrict__ dst, float* __restrict__ sums, int span, unsigned col_blocks) {
+  __shared__ float red[3][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)(blockIdx.x % col_blocks) * 512 + lane * 8;
+  const unsigned part = blockIdx.x / col_blocks;
+  const int64_t ld = (g.O + 31) / 32 * 32, rows32 = (g.R + 31) / 32 * 32;
+  const int64_t r1 = min(rows32, (int64_t)(part + 1) * span);
+  const TO* gy = static_cast<const TO*>(g.grad_y);
+  const TO* z = static_cast<const TO*>(g.preact_in);
+  const bool vec = ((((uintptr_t)gy) | ((uintptr_t)z) | (uintptr_t)(g.O * sizeof(TO))) & 15) == 0;
+  float s[8] = {};
+  if (c < ld) {
+    for (int64_t r = (int64_t)part * span + wave; r < r1; r += 4) {
+      float d[8];
+      eight<TO>(gy, g.R, g.O, r, c, vec, d);
+      if (g.act != SPCFG_ACT_NONE) {
+        float y[8];
+        eight<TO>(z, g.R, g.O, r, c, vec, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] *= act_slope(g.act, y[i]);
+      }
+      if (dst) put_planes(dst + r * ld + c, rows32 * ld, d, TI());
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += d[i];
+    }
+  }
+  if (!sums) return;
+  if (wave) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[wave - 1][lane * 8 + i] = s[i];
+  }
+  __syncthreads();
+  if (wave == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < g.O) sums[(int64_t)part * g.O + c + i] = ((s[i] + red[0][lane * 8 + i]) + red[1][lane * 8 + i]) + red[2][lane * 8 + i];
+  }
+}
+
+// ---- which form, and what it needs -----------------------------------------------------------------------------------------
+struct Form { int bm, bn, tiles_m, tiles_n, steps, splits, per; };
+
+// splits: enough workgroups for all CUs, of at least 8 steps each
+Form form_of(int64_t M, int64_t N, int64_t K, bool fp32) {
+  Form f;
+  const int steps = (int)((K + BK - 1) / BK);
+  auto tiles = [](int64_t n, int t) { return (n + t - 1) / t; };
+  f.bm = 128;
+  f.bn = 128;
+  if (!fp32 && tiles(M, 256) * tiles(N, 256) >= 256 && K >= 2048) f.bm = f.bn = 256;
+  f.tiles_m = (int)tiles(M, f.bm);
+  f.tiles_n = (int)tiles(N, f.bn);
+  f.steps = steps;
+  const int64_t t = (int64_t)f.tiles_m * f.tiles_n, room = fp32 ? 256 : 512;
+  int64_t sp = t >= room / 2 ? 1 : room / t;
+  if (sp > steps / 8) sp = steps / 8;
+  if (sp < 1) sp = 1;
+  f.per = (int)((steps + sp - 1) / sp);
+  f.splits = (steps + f.per - 1) / f.per;
+  return f;
+}
+
+bool large(int64_t R, int64_t I, int64_t O) { return R * I * O >= ((int64_t)1 << 28) && R >= 64 && I >= 64 && O >= 64; }
+
+struct Plan {
+  bool on;                 // whether the layer takes tiled products at all
+  bool cut;                // x and W as planes (fp32, or rows that do not lie on 16 bytes)
+  bool dz;                 // dz as planes
+  int pl;
+  int64_t x, w, z;         // elements of one plane of x, W, dz
+  int span, parts;         // rows of a part of the bias's gradient
+  Form fwd, dx, dw;
+  size_t off_x, off_w, off_z, off_sums, off_part, bytes;
+};
+
+Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
+  Plan p{};
+  p.on = R > 0 && large(R, I, O);
+  if (!p.on) return p;
+  const bool fp32 = in_type == SPCFG_TYPE_F32;
+  p.pl = fp32 ? 3 : 1;
+  p.cut = fp32 || I % 8 != 0;
+  p.dz = fp32 || out_type == SPCFG_TYPE_F32 || act != SPCFG_ACT_NONE || O % 8 != 0;
+  p.x = up32(R) * up32(I);
+  p.w = up32(O) * up32(I);
+  p.z = up32(R) * up32(O);
+  const int64_t cb = (up32(O) + 511) / 512;
+  int64_t span = (up32(R) * cb / 1024 + 31) / 32 * 32;
+  if (span < 32) span = 32;
+  p.span = (int)span;
+  p.parts = (int)((up32(R) + span - 1) / span);
+  p.fwd = form_of(R, O, I, fp32);
+  p.dx = form_of(R, I, O, fp32);
+  p.dw = form_of(O, I, R, fp32);
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
+  p.off_x = take(p.cut ? (size_t)p.x * 2 * p.pl : 0);
+  p.off_w = take(p.cut ? (size_t)p.w * 2 * p.pl : 0);
+  p.off_z = take(p.dz ? (size_t)p.z * 2 * p.pl : 0);
+  p.off_sums = take((size_t)p.parts * O * 4);
+  size_t part = 0;
+  auto partial = [&](const Form& f, int64_t M, int64_t N) {
+    const size_t n = f.splits > 1 ? (size_t)f.splits * M * N * 4 : 0;
+    if (n > part) part = n;
+  };
+  partial(p.fwd, R, O);
+  partial(p.dx, R, I);
+  partial(p.dw, O, I);
+  p.off_part = take(part);
+  p.bytes = at;
+  return p;
+}
+
+template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
+void launch(const Args& a, const Product& p, hipStream_t st) {
+  hipLaunchKernelGGL((k_dense_tile<S, TA, TB, TI, TO, FORM>), dim3(p.tiles_m * p.tiles_n * p.splits + p.bias_blocks), dim3(64 * S::NW), 0, st, a, p);
+}
+
+template <typename TI, typename TO, int FORM>
+void product(const Args& a, Product p, const Form& f, hipStream_t st) {
+  constexpr bool TA = FORM == DW, TB = FORM != FWD;
+  p.steps = f.steps;
+  p.steps_per_split = f.per;
+  p.splits = f.splits;
+  p.tiles_m = f.tiles_m;
+  p.tiles_n = f.tiles_n;
+  if constexpr (std::is_same<TI, float>::value) {
+    launch<Shape<3, 128, 128, 2, 2, 3>, TA, TB, TI, TO, FORM>(a, p, st);
+  } else {
+    if (f.bm == 256) launch<Shape<1, 256, 256, 2, 2, 4>, TA, TB, TI, TO, FORM>(a, p, st);
+    else launch<Shape<1, 128, 128, 2, 2, 4>, TA, TB, TI, TO, FORM>(a, p, st);
+  }
+  if (p.splits > 1) {
+    const int64_t blocks = (p.M * p.N + 255) / 256;
+    hipLaunchKernelGGL((k_dense_join<TI, TO, FORM>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a, p);
+  }
+}
+
+template <typename T> void cut(const void* x, uint16_t* px, int64_t R, const void* W, uint16_t* pw, int64_t O, int64_t I, hipStream_t st) {
+  auto blocks = [&](int64_t rows) { return (unsigned)((up32(rows) * up32(I) / 8 + 255) / 256); };
+  const unsigned b0 = x ? blocks(R) : 0, b1 = W ? blocks(O) : 0;
+  Cut c{{x, W}, {px, pw}, {R, O}, {I, I}, b0};
+  hipLaunchKernelGGL(k_dense_cut<T>, dim3(b0 + b1), dim3(256), 0, st, c);
+}
+
+template <typename TI, typename TO>
+void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
+  Product q{};
+  q.M = a.R;
+  q.N = a.O;
+  q.partial = reinterpret_cast<float*>(ws + p.off_part);
+  if (p.cut) {
+    uint16_t *px = reinterpret_cast<uint16_t*>(ws + p.off_x), *pw = reinterpret_cast<uint16_t*>(ws + p.off_w);
+    cut<TI>(a.x, px, a.R, a.W, pw, a.O, a.I, st);
+    q.A = px; q.B = pw; q.plane_a = p.x; q.plane_b = p.w;
+    q.lda = q.ldb = q.K = up32(a.I);
+  } else {
+    q.A = static_cast<const uint16_t*>(a.x); q.B = static_cast<const uint16_t*>(a.W);
+    q.lda = q.ldb = q.K = a.I;
+  }
+  product<TI, TO, FWD>(a, q, p.fwd, st);
+}
+
+template <typename TI, typename TO>
+void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
+  const uint16_t *x = static_cast<const uint16_t*>(a.x), *W = static_cast<const uint16_t*>(a.W);
+  const uint16_t* z = static_cast<const uint16_t*>(a.grad_y);
+  int64_t ldi = a.I, ldo = a.O;
+  bool kx = false, kz = false;  // whether rows are padded with zeros to a whole step
+  if (p.cut) {
+    uint16_t *px = reinterpret_cast<uint16_t*>(ws + p.off_x), *pw = reinterpret_cast<uint16_t*>(ws + p.off_w);
+    cut<TI>(a.grad_W ? a.x : nullptr, px, a.R, a.grad_x ? a.W : nullptr, pw, a.O, a.I, st);
+    x = px; W = pw; ldi = up32(a.I); kx = true;
+  }
+  float* sums = a.grad_bias ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
+  uint16_t* pz = p.dz ? reinterpret_cast<uint16_t*>(ws + p.off_z) : nullptr;
+  if (pz || sums) {
+    const unsigned cb = (unsigned)((up32(a.O) + 511) / 512);
+    hipLaunchKernelGGL((k_dense_dz<TI, TO>), dim3(cb * p.parts), dim3(256), 0, st, a, pz, sums, p.span, cb);
+  }
+  if (pz) { z = pz; ldo = up32(a.O); kz = true; }
+  Product q{};
+  q.partial = reinterpret_cast<float*>(ws + p.off_part);
+  if (a.grad_x) {
+    q.A = z; q.lda = ldo; q.plane_a = p.z;
+    q.B = W; q.ldb = ldi; q.plane_b = p.w;
+    q.M = a.R; q.N = a.I;
+    q.K = kz && kx ? up32(a.O) : a.O;
+    product<TI, TO, DX>(a, q, p.dx, st);
+  }
+  if (a.grad_W) {
+    q.A = z; q.lda = ldo; q.plane_a = p.z;
+    q.B = x; q.ldb = ldi; q.plane_b = p.x;
+    q.M = a.O; q.N = a.I;
+    q.K = kz && kx ? up32(a.R) : a.R;
+    q.bias_part = sums;
+    q.bias_parts = p.parts;
+    q.bias_blocks = sums ? (int)((a.O + 63) / 64) : 0;
+    product<TI, TO, DW>(a, q, p.dw, st);
+  }
+}
+
+}  // namespace
+
+size_t tiled_workspace(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
+  return plan_of(R, I, O, in_type, out_type, act).bytes;
+}
+
+bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st) {
+  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act);
+  if (!p.on || (!p.cut && (!on16(a.x) || !on16(a.W)))) return false;
+  char* w = static_cast<char*>(ws);
+  if (in_type == SPCFG_TYPE_F32) forward<float, float>(a, p, w, st);
+  else if (out_type == SPCFG_TYPE_F32) forward<uint16_t, float>(a, p, w, st);
+  else forward<uint16_t, uint16_t>(a, p, w, st);
+  return true;
+}
+
+bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st) {
+  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act);
+  if (!p.on || (!p.cut && (!on16(a.x) || !on16(a.W))) || (!p.dz && !on16(a.grad_y))) return false;
+  char* w = static_cast<char*>(ws);
+  if (in_type == SPCFG_TYPE_F32) backward<float, float>(a, p, w, st);
+  else if (out_type == SPCFG_TYPE_F32) backward<uint16_t, float>(a, p, w, st);
+  else backward<uint16_t, uint16_t>(a, p, w, st);
+  return true;
+}
+
+}  // namespace dense
+}  // namespace spcfg

@@ -147,6 +147,44 @@ def test_larger(R, I, O, types):
 
 
 @pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_wide(types):
+    """More tiles than CUs and long sums; the reference is 64-bit arithmetic on the GPU, over a sample of rows and columns."""
+    import torch
+    R, I, O = 4100, 2056, 4104
+    print("case dense wide", types, flush=True)
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(7)
+    n = lambda *s: torch.randn(*s, generator=g, device="cuda:0")
+    ti, to = d_of(types[0]), d_of(types[1])
+    x, W, b = n(R, I).to(ti), (n(O, I) * 0.02).to(ti), n(O).to(ti)
+    r, gy = n(R, O).to(to), n(R, O).to(to)
+    cfg = bd.make_dense_config(R, I, O, t_of(types[0]), t_of(types[1]), bd.ACT_RELU)
+    ws = workspace(cfg)
+    y, z = torch.empty(R, O, dtype=to, device="cuda:0"), torch.empty(R, O, dtype=to, device="cuda:0")
+    bd.spcfg_dense_forward(cfg, x, W, b, r, y, z, ws)
+    gx, gW, gb = (torch.full(s, float("nan"), dtype=ti, device="cuda:0") for s in ((R, I), (O, I), (O,)))
+    bd.spcfg_dense_backward(cfg, x, W, z, gy, None, gx, gW, gb, ws)
+    rows = torch.cat([torch.arange(0, R, 37), torch.arange(R - 5, R)]).cuda()
+    cols = torch.cat([torch.arange(0, O, 41), torch.arange(O - 5, O)]).cuda()
+    D = lambda t: t.double()
+    want_z = D(x)[rows] @ D(W).t() + D(b)
+    q = torch.sqrt((D(x)[rows] ** 2) @ (D(W) ** 2).t())
+    ez = (U * (16 + 6 * I / 16) * 2 * q + 2.0 ** -21 * (want_z.abs() + D(b).abs())).cpu().numpy()
+    close("preact", values(z[rows]), want_z.cpu().numpy(), ez + half_step(types[1]) * want_z.abs().cpu().numpy())
+    want = want_z.clamp(min=0) + D(r)[rows]
+    close("y", values(y[rows]), want.cpu().numpy(), ez + (2.0 ** -21 + half_step(types[1])) * want.abs().cpu().numpy())
+    dz = D(gy) * (D(z) > 0)
+    lossy = 4 * 2.0 ** -8 if types[0] == "bf16" else 0.0
+    for name, got, A, B, K in (("grad_x", gx[rows], dz[rows], D(W), O), ("grad_W", gW[cols], dz[:, cols].t(), D(x), R)):
+        want, q = A @ B, torch.sqrt((A ** 2) @ (B ** 2))
+        tol = (U * (16 + 6 * K / 16) * 2 + lossy) * q + (half_step(types[0]) + 2.0 ** -22) * want.abs()
+        close(name, values(got), want.cpu().numpy(), tol.cpu().numpy())
+    want, q = dz.sum(0), torch.sqrt((dz ** 2).sum(0))
+    close("grad_bias", values(gb), want.cpu().numpy(),
+          (U * (16 + 6 * R / 16) * 2 * q + (half_step(types[0]) + 2.0 ** -22) * want.abs()).cpu().numpy())
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
 @pytest.mark.parametrize("R,I,O", [(70, 64, 96), (1200, 520, 1040)])
 def test_options_and_alignments(R, I, O, types):
     print("case dense options", R, I, O, types, flush=True)
