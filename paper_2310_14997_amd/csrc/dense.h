@@ -56,25 +56,111 @@ struct Args {
 // The three products of a layer: z = x W^T, dx = dz W, dW = dz^T x.
 enum { FWD = 0, DX = 1, DW = 2 };
 
-// Epilogue of one element (m, n) of a product, whose sum is s.
-template <typename TI, typename TO, int FORM>
-__device__ __forceinline__ void store_one(const Args& g, int64_t m, int64_t n, float s) {
-  const int64_t at = m * (FORM == FWD ? g.O : g.I) + n;
-  if constexpr (FORM == FWD) {
-    if (g.bias) s += to_float<TI>(static_cast<const TI*>(g.bias)[n]);
-    if (g.preact) static_cast<TO*>(g.preact)[at] = from_float<TO>(s);
-    s = act_value(g.act, s);
-    if (g.residual) s += to_float<TO>(static_cast<const TO*>(g.residual)[at]);
-    static_cast<TO*>(g.y)[at] = from_float<TO>(s);
-  } else if constexpr (FORM == DX) {
-    if (g.grad_x_add) s += to_float<TI>(static_cast<const TI*>(g.grad_x_add)[at]);
-    static_cast<TI*>(g.grad_x)[at] = from_float<TI>(s);
+// N values of T as one access of N * sizeof(T) bytes
+template <typename T, int N> __device__ __forceinline__ void get(const T* p, float (&v)[N]) {
+  typedef T V __attribute__((ext_vector_type(N)));
+  T x[N];
+  const V w = *reinterpret_cast<const V*>(p);
+  __builtin_memcpy(x, &w, sizeof(x));
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = to_float<T>(x[i]);
+}
+template <typename T, int N> __device__ __forceinline__ void put(T* p, const float (&v)[N]) {
+  typedef T V __attribute__((ext_vector_type(N)));
+  T x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = from_float<T>(v[i]);
+  V w;
+  __builtin_memcpy(&w, x, sizeof(x));
+  *reinterpret_cast<V*>(p) = w;
+}
+
+template <typename T> __device__ __forceinline__ void get8(const T* p, float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    get<T, 8>(p, v);
   } else {
-    TI* o = static_cast<TI*>(g.grad_W) + at;
-    if (g.accumulate) s += to_float<TI>(*o);
-    *o = from_float<TI>(s);
+    float a[4], b[4];
+    get<T, 4>(p, a);
+    get<T, 4>(p + 4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[i + 4] = b[i]; }
   }
 }
+template <typename T> __device__ __forceinline__ void put8(T* p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    put<T, 8>(p, v);
+  } else {
+    put<T, 4>(p, {v[0], v[1], v[2], v[3]});
+    put<T, 4>(p + 4, {v[4], v[5], v[6], v[7]});
+  }
+}
+
+// What becomes of a product's sums, one by one or eight adjacent ones of a row (16 bytes at a time where everything involved
+// lies on 16).
+template <typename TI, typename TO, int FORM> struct Epilogue {
+  int act, accumulate;
+  const TI *bias, *add;
+  const TO* residual;
+  TO *y, *preact;
+  TI* o;
+  bool vec;
+  __device__ __forceinline__ Epilogue(const Args& g, int64_t N)
+      : act(g.act), accumulate(g.accumulate), bias(static_cast<const TI*>(g.bias)), add(static_cast<const TI*>(g.grad_x_add)),
+        residual(static_cast<const TO*>(g.residual)), y(static_cast<TO*>(g.y)), preact(static_cast<TO*>(g.preact)),
+        o(static_cast<TI*>(FORM == DX ? g.grad_x : g.grad_W)) {
+    const uintptr_t at = FORM == FWD ? (uintptr_t)y | (uintptr_t)preact | (uintptr_t)residual
+                                     : (uintptr_t)o | (FORM == DX ? (uintptr_t)add : 0);
+    vec = ((at | (uintptr_t)(N * (FORM == FWD ? sizeof(TO) : sizeof(TI)))) & 15) == 0;
+  }
+  __device__ __forceinline__ float bias_of(int64_t n, int64_t N) const {
+    return FORM == FWD && bias && n < N ? to_float<TI>(bias[n]) : 0.0f;
+  }
+  __device__ __forceinline__ void one(int64_t at, float s, float b) const {
+    if constexpr (FORM == FWD) {
+      s += b;
+      if (preact) preact[at] = from_float<TO>(s);
+      s = act_value(act, s);
+      if (residual) s += to_float<TO>(residual[at]);
+      y[at] = from_float<TO>(s);
+    } else if constexpr (FORM == DX) {
+      if (add) s += to_float<TI>(add[at]);
+      o[at] = from_float<TI>(s);
+    } else {
+      if (accumulate) s += to_float<TI>(o[at]);
+      o[at] = from_float<TI>(s);
+    }
+  }
+  __device__ __forceinline__ void eight(int64_t at, float (&s)[8], const float (&b)[8], int64_t left) const {
+    if (!vec || left < 8) {
+      for (int u = 0; u < 8; ++u)
+        if (u < left) one(at + u, s[u], b[u]);
+      return;
+    }
+    float r[8];
+    if constexpr (FORM == FWD) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s[u] += b[u];
+      if (preact) put8<TO>(preact + at, s);
+      if (act != SPCFG_ACT_NONE) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[u] = act_value(act, s[u]);
+      }
+      if (residual) {
+        get8<TO>(residual + at, r);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[u] += r[u];
+      }
+      put8<TO>(y + at, s);
+    } else {
+      if (FORM == DX ? add != nullptr : accumulate != 0) {
+        get8<TI>(FORM == DX ? add + at : o + at, r);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[u] += r[u];
+      }
+      put8<TI>(o + at, s);
+    }
+  }
+};
 template <typename TI>
 __device__ __forceinline__ void store_bias(const Args& g, int64_t m, float s) {
   TI* o = static_cast<TI*>(g.grad_bias) + m;

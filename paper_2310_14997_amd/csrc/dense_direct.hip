@@ -176,13 +176,14 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
     for (int i = 0; i < MT; ++i) bl[(wave * MT + i) * 64 + lane] = bsum[i];
   }
   __syncthreads();
+  const Epilogue<TI, TO, FORM> ep(g, N);
   for (int e = threadIdx.x; e < kTile; e += 64 * kWaves) {
     const int64_t m = m0 + e / (32 * NT), n = n0 + e % (32 * NT);
     if (m >= M || n >= N) continue;
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) s += lds[w * kTile + e];
-    store_one<TI, TO, FORM>(g, m, n, s);
+    ep.one(m * N + n, s, ep.bias_of(n, N));
   }
   if (FORM == DW && g.grad_bias && tn == 0 && threadIdx.x < 32 * MT) {
     const int64_t m = m0 + threadIdx.x;

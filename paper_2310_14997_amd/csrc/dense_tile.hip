@@ -70,6 +70,31 @@ template <int PL_, int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
 
 #define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
 
+// eight floats of a row of which `left` are there; vec: rows lie on 16 bytes
+__device__ __forceinline__ void put_floats(float* p, const float (&s)[8], int64_t left, bool vec) {
+  if (vec && left >= 8) {
+    put<float, 4>(p, {s[0], s[1], s[2], s[3]});
+    put<float, 4>(p + 4, {s[4], s[5], s[6], s[7]});
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (u < left) p[u] = s[u];
+  }
+}
+__device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_t left, bool vec) {
+  if (vec && left >= 8) {
+    float a[4], b[4];
+    get<float, 4>(p, a);
+    get<float, 4>(p + 4, b);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) { s[u] += a[u]; s[u + 4] += b[u]; }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (u < left) s[u] += p[u];
+  }
+}
+
 template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
 __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW / 4 : S::NW / 4) k_dense_tile(Args g, Product p) {
   constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS;
@@ -105,41 +130,72 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
     t = xcd * q + min(xcd, r) + (b >> 3);
   }
   const unsigned per_split = p.tiles_m * p.tiles_n;
-  const int split = t / per_split;
+  const int split = __builtin_amdgcn_readfirstlane(t / per_split);
   t -= split * per_split;
   const unsigned band = t / (8 * p.tiles_n), rows_here = min(8u, p.tiles_m - band * 8), in_band = t - band * 8 * p.tiles_n;
-  const int64_t m0 = (int64_t)(band * 8 + in_band % rows_here) * S::BM, n0 = (int64_t)(in_band / rows_here) * S::BN;
+  // (divisions are done in vector registers: back to scalar ones, where everything that depends on the tile alone stays)
+  const int tile_m = __builtin_amdgcn_readfirstlane(band * 8 + in_band % rows_here);
+  const int tile_n = __builtin_amdgcn_readfirstlane(in_band / rows_here);
+  const int64_t m0 = (int64_t)tile_m * S::BM, n0 = (int64_t)tile_n * S::BN;
   const int k0 = split * p.steps_per_split, k1 = min(p.steps, k0 + p.steps_per_split);
 
   // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 bytes; across: 4 of 256.
+  // Addresses are a base per operand and plane, the same for all lanes, plus 32 bits (the host checks that these do).
   const unsigned lds0 = lds_address(lds);
-  const unsigned char* gp[ND];
-  unsigned e_lds[ND];
+  unsigned e_off[ND], e_lds[ND];
   const int r_al = lane >> 2, c_al = (lane & 3) ^ ((lane >> 4) & 3);  // row of the 16, and piece: XOR with bits 2..3 of the row
   const int r_ac = lane >> 4, c_ac = (((lane & 15) >> 2) ^ r_ac) * 32 + (lane & 3) * 8;
-  const int64_t step_a = TA ? 2 * BK * p.lda : 2 * BK, step_b = TB ? 2 * BK * p.ldb : 2 * BK;  // bytes a step
   static_for<0, ND>([&](auto j) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
     constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
     const int q = wave + e0 % per;
     e_lds[jv] = (unsigned)((isA ? plane * S::PTA : PL * S::PTA + plane * S::PTB) + q * 1024);
-    const uint16_t* base = isA ? p.A + plane * p.plane_a : p.B + plane * p.plane_b;
     const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
-    if (isA ? TA : TB) {
-      const int64_t col = min(o0 + (q >> 3) * 128 + c_ac, (len + 7) / 8 * 8 - 8);
-      gp[jv] = reinterpret_cast<const unsigned char*>(base + (4 * (q & 7) + r_ac) * ld + col);
+    if constexpr (isA ? TA : TB) {
+      const int64_t col = min(o0 + (q >> 3) * 128 + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
+      e_off[jv] = (unsigned)(2 * ((4 * (q & 7) + r_ac) * ld + col));
     } else {
-      gp[jv] = reinterpret_cast<const unsigned char*>(base + min(o0 + 16 * q + r_al, len - 1) * ld + c_al * 8);
+      e_off[jv] = (unsigned)(2 * (min(o0 + 16 * q + r_al, len - 1) - o0) * ld + 16 * c_al);
     }
   });
-  auto load_one = [&](auto j, unsigned stage, int kt) {
+  const int64_t step_a = TA ? 2 * BK * p.lda : 2 * BK, step_b = TB ? 2 * BK * p.ldb : 2 * BK;  // bytes a step
+  const unsigned char* base[2][PL];  // of the step that is loaded next
+  static_for<0, PL>([&](auto pl) {
+    constexpr int v = decltype(pl)::value;
+    base[0][v] = reinterpret_cast<const unsigned char*>(p.A + v * p.plane_a + (TA ? m0 : m0 * p.lda)) + k0 * step_a;
+    base[1][v] = reinterpret_cast<const unsigned char*>(p.B + v * p.plane_b + (TB ? n0 : n0 * p.ldb)) + k0 * step_b;
+    // (opaque: otherwise they are computed anew from kernel arguments inside the loop, and waiting for those waits for
+    // operand reads as well)
+    asm volatile("" : "+s"(base[0][v]), "+s"(base[1][v]));
+  });
+  int64_t by_a = step_a, by_b = step_b;
+  asm volatile("" : "+s"(by_a), "+s"(by_b));
+  auto load_one = [&](auto j, unsigned stage) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
-    constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA);
-    const int64_t k = (int64_t)kt * BK + ((isA ? TA : TB) ? 4 * ((wave + e0 % per) & 7) + r_ac : c_al * 8);
-    const unsigned char* at = gp[jv] + kt * (isA ? step_a : step_b);
-    dma16(k < p.K ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
+    constexpr int plane = S::NW * (isA ? jv : jv - S::NDA) / ((isA ? S::BM : S::BN) / 16);
+    dma16(base[isA ? 0 : 1][plane] + e_off[jv], lds0 + stage + e_lds[jv]);
+  };
+  auto advance = [&]() {
+#pragma unroll
+    for (int v = 0; v < PL; ++v) {
+      base[0][v] += by_a;
+      base[1][v] += by_b;
+    }
+  };
+  // the last step of all where k ends inside it: what lies beyond reads as zero
+  const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * BK);  // k of the last step, 1 .. 32
+  const int whole = last_left < BK ? p.steps - 1 : p.steps;        // steps that are whole
+  auto load_last = [&](unsigned stage) {
+    static_for<0, ND>([&](auto j) {
+      constexpr int jv = decltype(j)::value;
+      constexpr bool isA = jv < S::NDA;
+      constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
+      const int k = (isA ? TA : TB) ? 4 * ((wave + e0 % per) & 7) + r_ac : c_al * 8;
+      const unsigned char* at = base[isA ? 0 : 1][plane] + e_off[jv];
+      dma16(k < last_left ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
+    });
   };
 
   // operand reads: byte offsets inside a stage of the fragments of the first 16 k of plane 0
@@ -228,7 +284,11 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   const int n = k1 - k0;
   static_for<0, NS>([&](auto s) {
     constexpr int sv = decltype(s)::value;
-    if (sv < n) static_for<0, ND>([&](auto j) { load_one(j, sv * S::STAGE, k0 + sv); });
+    if (sv < n) {
+      if (k0 + sv < whole) static_for<0, ND>([&](auto j) { load_one(j, sv * S::STAGE); });
+      else load_last(sv * S::STAGE);
+      advance();
+    }
   });
   if (n >= NS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND * (NS - 1)) : "memory");
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -262,7 +322,9 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     SPCFG_SB
-    const bool more = i + NS < n;
+    const bool more = i + NS < n && k0 + i + NS < whole;
+    if (i + NS < n && k0 + i + NS >= whole) load_last(cur);
+    SPCFG_SB
     static_for<NB, NM>([&](auto m) {
       constexpr int s = decltype(m)::value - NB;
       mfma_one(Y, m);
@@ -273,40 +335,65 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
       });
       if (more) {
         static_for<0, ND>([&](auto j) {
-          if constexpr ((decltype(j)::value * RS) / ND == s) load_one(j, cur, k0 + i + NS);
+          if constexpr ((decltype(j)::value * RS) / ND == s) load_one(j, cur);
         });
       }
       SPCFG_SB
     });
+    advance();
     cur = nxt;
   }
   wait_reads(X);  // (the last step read ahead into a place without new data: nothing of it is used)
 
-  // accumulators of a 32 x 32 tile: column lane % 32, row 8 (v / 4) + 4 (lane / 32) + v % 4
-  const int64_t mw = m0 + wm * MI * 32 + 4 * (lane >> 5), nw = n0 + wn * NI * 32 + (lane & 31);
+  // Epilogue: 32 rows of a wavefront at a time go through its own part of LDS, from the accumulators' order (32 x 32 tile: column
+  // lane % 32, row 8 (v / 4) + 4 (lane / 32) + v % 4) to eight adjacent columns a lane.  Rows there are 32 NI + 8 floats
+  // apart: the two halves of a wavefront write rows four apart, in different banks.
+  constexpr int LR = 32 * NI + 8, PER_ROW = 4 * NI, ROWS = 64 / PER_ROW;  // lanes of a row, rows at a time
+  static_assert(S::NW * 32 * LR * 4 <= S::kLds, "the epilogue's rows fit");
+  __syncthreads();  // (nobody reads operands any more)
+  float* out = reinterpret_cast<float*>(lds) + wave * 32 * LR;
+  const int64_t mw = m0 + wm * MI * 32 + lane / PER_ROW, c = n0 + wn * NI * 32 + lane % PER_ROW * 8;
+  const Epilogue<TI, TO, FORM> ep(g, p.N);
+  float* part = p.splits > 1 ? p.partial + (int64_t)split * p.M * p.N : nullptr;
+  float bias[8];
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
+  for (int u = 0; u < 8; ++u) bias[u] = ep.bias_of(c + u, p.N);
+  static_for<0, MI>([&](auto i) {
+    constexpr int mi = decltype(i)::value;
+    static_for<0, 16 * NI>([&](auto w) {
+      constexpr int v = decltype(w)::value / NI, ni = decltype(w)::value % NI;
+      out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * LR + ni * 32 + (lane & 31)] = acc[mi][ni][v];
+    });
+    // (a wavefront's own accesses to LDS are in order; the fences keep the compiler's)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int r = 0; r < 32; r += ROWS) {
+      const int64_t m = mw + mi * 32 + r;
+      const float* from = out + (r + lane / PER_ROW) * LR + lane % PER_ROW * 8;
+      float s[8];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int64_t m = mw + mi * 32 + 8 * (v >> 2) + (v & 3);
-      if (m >= p.M) continue;
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
-        const int64_t c = nw + ni * 32;
-        if (c >= p.N) continue;
-        if (p.splits > 1) p.partial[((int64_t)split * p.M + m) * p.N + c] = acc[mi][ni][v];
-        else store_one<TI, TO, FORM>(g, m, c, acc[mi][ni][v]);
-      }
+      for (int u = 0; u < 8; ++u) s[u] = from[u];
+      if (m >= p.M || c >= p.N) continue;
+      if (part) put_floats(part + m * p.N + c, s, p.N - c, (p.N & 3) == 0);
+      else ep.eight(m * p.N + c, s, bias, p.N - c);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  });
 }
 
+// Partial tiles added up in the order of their k, eight columns a thread.
 template <typename TI, typename TO, int FORM>
 __global__ void __launch_bounds__(256) k_dense_join(Args g, Product p) {
-  const int64_t n = p.M * p.N;
+  const int64_t per_row = (p.N + 7) / 8, n = p.M * per_row, all = p.M * p.N;
+  const Epilogue<TI, TO, FORM> ep(g, p.N);
+  const bool vec = (p.N & 3) == 0;
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
-    float s = p.partial[e];
-    for (int q = 1; q < p.splits; ++q) s += p.partial[(int64_t)q * n + e];
-    store_one<TI, TO, FORM>(g, e / p.N, e % p.N, s);
+    const int64_t m = e / per_row, c = (e - m * per_row) * 8;
+    float s[8] = {}, bias[8];
+#pragma unroll 4
+    for (int q = 0; q < p.splits; ++q) add_floats(p.partial + q * all + m * p.N + c, s, p.N - c, vec);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) bias[u] = ep.bias_of(c + u, p.N);
+    ep.eight(m * p.N + c, s, bias, p.N - c);
   }
 }
 
@@ -432,7 +519,10 @@ Form form_of(int64_t M, int64_t N, int64_t K, bool fp32) {
   return f;
 }
 
-bool large(int64_t R, int64_t I, int64_t O) { return R * I * O >= ((int64_t)1 << 28) && R >= 64 && I >= 64 && O >= 64; }
+bool large(int64_t R, int64_t I, int64_t O) {
+  const int64_t most = 1 << 22;  // offsets inside a tile (256 rows, or 32 rows across k) fit 32 bits
+  return R * I * O >= ((int64_t)1 << 28) && R >= 64 && I >= 64 && O >= 64 && R < most && I < most && O < most;
+}
 
 struct Plan {
   bool on;                 // whether the layer takes tiled products at all
@@ -503,7 +593,7 @@ void product(const Args& a, Product p, const Form& f, hipStream_t st) {
     else launch<Shape<1, 128, 128, 2, 2, 4>, TA, TB, TI, TO, FORM>(a, p, st);
   }
   if (p.splits > 1) {
-    const int64_t blocks = (p.M * p.N + 255) / 256;
+    const int64_t blocks = (p.M * ((p.N + 7) / 8) + 255) / 256;
     hipLaunchKernelGGL((k_dense_join<TI, TO, FORM>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a, p);
   }
 }
