@@ -252,30 +252,54 @@ def spcfg_rules_backward(log_root, L, R, emis_logits, emis_lse, tokens, lengths,
         _dev(grad_emis_logits, "grad_emis_logits", (P, V)), _dev(scratch, "scratch", (32, P)), _stream()))
 
 
-def _here(t, name, shape, type=TYPE_F32, dtype=None):
-    """Pointer of a tensor on torch's current device, of the given element type and shape; None stays None."""
-    import torch
+_torch = None
+_F32 = _I32 = _U8 = None
+_FLOATS = ()  # by SPCFG_TYPE_*
+_current_device = _raw_stream = None
+
+
+def _device():
+    """The current device; -2 where there is none.  The layers and losses are small calls, often: what follows is written to cost
+    little where the arguments are in order, and says what is wrong with them where they are not."""
+    global _torch, _F32, _I32, _U8, _FLOATS, _current_device, _raw_stream
+    if _torch is None:
+        import torch
+        _F32, _I32, _U8, _FLOATS = torch.float32, torch.int32, torch.uint8, (torch.float32, torch.bfloat16)
+        # what torch's generated code uses for the two, without the checks of the public functions (0.1 us against 0.7 and 3)
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        _torch = torch
+    try:
+        return _current_device()
+    except RuntimeError:
+        return -2
+
+
+def _refuse(t, name, shape, dtype, dev):
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
+        raise TypeError(f"{name} must be a contiguous {dtype} device tensor")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    raise ValueError(f"{name} is on {t.device}, not on the current device {dev}")
+
+
+def _here(t, name, shape, dtype, dev):
+    """Pointer of a contiguous tensor of that element type and shape on device `dev`; None stays None."""
     if t is None:
         return None
-    dtype = dtype or (torch.bfloat16 if type == TYPE_BF16 else torch.float32)
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.dtype == dtype):
-        raise TypeError(f"{name} must be a contiguous {dtype} device tensor")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device {torch.cuda.current_device()}")
+    if not (isinstance(t, _torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape
+            and t.is_contiguous()):
+        _refuse(t, name, shape, dtype, dev)
     return t.data_ptr()
 
 
-def _scratch(workspace):
+def _scratch(t, dev):
     """(pointer, bytes) of a workspace tensor; None where no workspace is needed."""
-    import torch
-    if workspace is None:
+    if t is None:
         return None, 0
-    ptr, n = _ws(workspace)
-    if workspace.device.index != torch.cuda.current_device():
-        raise ValueError(f"workspace is on {workspace.device}, not on the current device {torch.cuda.current_device()}")
-    return ptr, n
+    if not (isinstance(t, _torch.Tensor) and t.dtype is _U8 and t.get_device() == dev and t.is_contiguous()):
+        _refuse(t, "workspace", None, _U8, dev)
+    return t.data_ptr(), t.numel()
 
 
 def make_dense_config(rows, n_in, n_out, in_type=TYPE_F32, out_type=TYPE_F32, activation=ACT_NONE, flags=0):
@@ -289,33 +313,35 @@ def spcfg_dense_workspace_bytes(cfg):
     return out.value
 
 
+def _dense_types(cfg):
+    if cfg.in_type not in (0, 1) or cfg.out_type not in (0, 1):
+        _check(-5)
+    return _FLOATS[cfg.in_type], _FLOATS[cfg.out_type]
+
+
 def spcfg_dense_forward(cfg, x, W, bias, residual, y, preact, workspace):
     """y = act(x W^T + bias) + residual (see include/spcfg.h); bias, residual and preact may be None."""
-    R, I, O, ti, to = cfg.rows, cfg.n_in, cfg.n_out, cfg.in_type, cfg.out_type
-    wp, wb = _scratch(workspace)
+    dev = _device()
+    ti, to = _dense_types(cfg)
+    xs, ys = (cfg.rows, cfg.n_in), (cfg.rows, cfg.n_out)
+    wp, wb = _scratch(workspace, dev)
     _check(load().spcfg_dense_forward(
-        C.byref(cfg), _here(x, "x", (R, I), ti), _here(W, "W", (O, I), ti), _here(bias, "bias", (O,), ti),
-        _here(residual, "residual", (R, O), to), _here(y, "y", (R, O), to), _here(preact, "preact", (R, O), to), wp, wb,
-        _stream()))
+        C.byref(cfg), _here(x, "x", xs, ti, dev), _here(W, "W", (cfg.n_out, cfg.n_in), ti, dev),
+        _here(bias, "bias", (cfg.n_out,), ti, dev), _here(residual, "residual", ys, to, dev), _here(y, "y", ys, to, dev),
+        _here(preact, "preact", ys, to, dev), wp, wb, _raw_stream(dev)))
 
 
 def spcfg_dense_backward(cfg, x, W, preact, grad_y, grad_x_add, grad_x, grad_W, grad_bias, workspace):
     """Gradients of spcfg_dense_forward; those that are None are not computed."""
-    R, I, O, ti, to = cfg.rows, cfg.n_in, cfg.n_out, cfg.in_type, cfg.out_type
-    wp, wb = _scratch(workspace)
+    dev = _device()
+    ti, to = _dense_types(cfg)
+    xs, ws, ys = (cfg.rows, cfg.n_in), (cfg.n_out, cfg.n_in), (cfg.rows, cfg.n_out)
+    wp, wb = _scratch(workspace, dev)
     _check(load().spcfg_dense_backward(
-        C.byref(cfg), _here(x, "x", (R, I), ti), _here(W, "W", (O, I), ti), _here(preact, "preact", (R, O), to),
-        _here(grad_y, "grad_y", (R, O), to), _here(grad_x_add, "grad_x_add", (R, I), ti),
-        _here(grad_x, "grad_x", (R, I), ti), _here(grad_W, "grad_W", (O, I), ti),
-        _here(grad_bias, "grad_bias", (O,), ti), wp, wb, _stream()))
-
-
-def _scores_type(logits):
-    import torch
-    types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
-    if not isinstance(logits, torch.Tensor) or logits.dtype not in types or logits.dim() != 2:
-        raise TypeError("logits must be a two-dimensional float32 or bfloat16 device tensor")
-    return types[logits.dtype]
+        C.byref(cfg), _here(x, "x", xs, ti, dev), _here(W, "W", ws, ti, dev), _here(preact, "preact", ys, to, dev),
+        _here(grad_y, "grad_y", ys, to, dev), _here(grad_x_add, "grad_x_add", xs, ti, dev),
+        _here(grad_x, "grad_x", xs, ti, dev), _here(grad_W, "grad_W", ws, ti, dev),
+        _here(grad_bias, "grad_bias", (cfg.n_out,), ti, dev), wp, wb, _raw_stream(dev)))
 
 
 def spcfg_distill_workspace_bytes(rows, V):
@@ -325,67 +351,80 @@ def spcfg_distill_workspace_bytes(rows, V):
 
 
 def _distill_inputs(logits, teacher_logits, teacher_ids, temperature):
-    import torch
-    type = _scores_type(logits)
-    (rows, V), k = logits.shape, teacher_ids.shape[-1]
-    return type, rows, V, k, [
-        type, rows, V, k, _here(logits, "logits", (rows, V), type), _here(teacher_logits, "teacher_logits", (rows, k), type),
-        _here(teacher_ids, "teacher_ids", (rows, k), dtype=torch.int32), float(temperature)]
+    """(device, dtype, rows, V, the call's first arguments)"""
+    dev = _device()
+    dtype = getattr(logits, "dtype", None)
+    if not isinstance(logits, _torch.Tensor) or dtype not in _FLOATS or logits.dim() != 2:
+        raise TypeError("logits must be a two-dimensional float32 or bfloat16 device tensor")
+    if not isinstance(teacher_ids, _torch.Tensor) or teacher_ids.dim() != 2:
+        raise TypeError("teacher_ids must be a two-dimensional int32 device tensor")
+    (rows, V), k = logits.shape, teacher_ids.shape[1]
+    return dev, dtype, rows, V, (
+        _FLOATS.index(dtype), rows, V, k, _here(logits, "logits", (rows, V), dtype, dev),
+        _here(teacher_logits, "teacher_logits", (rows, k), dtype, dev),
+        _here(teacher_ids, "teacher_ids", (rows, k), _I32, dev), float(temperature))
 
 
 def spcfg_distill_forward(logits, teacher_logits, teacher_ids, temperature, loss, lse, workspace):
     """Loss of every row of logits [rows, V] against a teacher's top entries [rows, k], and the rows' logsumexp."""
-    _, rows, _, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
-    wp, wb = _scratch(workspace)
-    _check(load().spcfg_distill_forward(*inputs, _here(loss, "loss", (rows,)), _here(lse, "lse", (rows,)), wp, wb, _stream()))
+    dev, _, rows, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    wp, wb = _scratch(workspace, dev)
+    _check(load().spcfg_distill_forward(*inputs, _here(loss, "loss", (rows,), _F32, dev), _here(lse, "lse", (rows,), _F32, dev),
+                                        wp, wb, _raw_stream(dev)))
 
 
 def spcfg_distill_backward(logits, teacher_logits, teacher_ids, temperature, lse, grad_loss, grad_logits):
     """Gradient of spcfg_distill_forward's losses, from the lse that it wrote."""
-    type, rows, V, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    dev, dtype, rows, V, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
     _check(load().spcfg_distill_backward(
-        *inputs, _here(lse, "lse", (rows,)), _here(grad_loss, "grad_loss", (rows,)),
-        _here(grad_logits, "grad_logits", (rows, V), type), _stream()))
+        *inputs, _here(lse, "lse", (rows,), _F32, dev), _here(grad_loss, "grad_loss", (rows,), _F32, dev),
+        _here(grad_logits, "grad_logits", (rows, V), dtype, dev), _raw_stream(dev)))
 
 
 def spcfg_distill_forward_backward(logits, teacher_logits, teacher_ids, temperature, grad_loss, loss, lse, grad_logits,
                                    workspace):
     """Loss and gradient in one call."""
-    type, rows, V, _, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
-    wp, wb = _scratch(workspace)
+    dev, dtype, rows, V, inputs = _distill_inputs(logits, teacher_logits, teacher_ids, temperature)
+    wp, wb = _scratch(workspace, dev)
     _check(load().spcfg_distill_forward_backward(
-        *inputs, _here(grad_loss, "grad_loss", (rows,)), _here(loss, "loss", (rows,)), _here(lse, "lse", (rows,)),
-        _here(grad_logits, "grad_logits", (rows, V), type), wp, wb, _stream()))
+        *inputs, _here(grad_loss, "grad_loss", (rows,), _F32, dev), _here(loss, "loss", (rows,), _F32, dev),
+        _here(lse, "lse", (rows,), _F32, dev), _here(grad_logits, "grad_logits", (rows, V), dtype, dev), wp, wb,
+        _raw_stream(dev)))
 
 
 def _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing):
-    import torch
+    """(device, B, pairs, the call's first arguments)"""
+    dev = _device()
+    for t, name in ((logZ, "logZ"), (chosen, "chosen")):
+        if not isinstance(t, _torch.Tensor) or t.dim() != 1:
+            raise TypeError(f"{name} must be a one-dimensional device tensor")
     (B,), (n,) = logZ.shape, chosen.shape
-    return B, n, [B, n, _here(logZ, "logZ", (B,)), _here(ref_logZ, "ref_logZ", (B,)),
-                  _here(chosen, "chosen", (n,), dtype=torch.int32), _here(rejected, "rejected", (n,), dtype=torch.int32),
-                  float(beta), float(smoothing)]
+    return dev, B, n, (
+        B, n, _here(logZ, "logZ", (B,), _F32, dev), _here(ref_logZ, "ref_logZ", (B,), _F32, dev),
+        _here(chosen, "chosen", (n,), _I32, dev), _here(rejected, "rejected", (n,), _I32, dev), float(beta), float(smoothing))
 
 
 def spcfg_preference_forward(logZ, ref_logZ, chosen, rejected, beta, smoothing, loss, margin):
     """Loss and margin of every pair of sentences (see include/spcfg.h); ref_logZ may be None."""
-    _, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
-    _check(load().spcfg_preference_forward(*inputs, _here(loss, "loss", (n,)), _here(margin, "margin", (n,)), _stream()))
+    dev, _, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    _check(load().spcfg_preference_forward(*inputs, _here(loss, "loss", (n,), _F32, dev),
+                                           _here(margin, "margin", (n,), _F32, dev), _raw_stream(dev)))
 
 
 def spcfg_preference_backward(logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, grad_logZ):
     """Gradient of the pairs' losses in logZ, as spcfg_inside_backward takes it."""
-    B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
-    _check(load().spcfg_preference_backward(*inputs, _here(grad_loss, "grad_loss", (n,)),
-                                            _here(grad_logZ, "grad_logZ", (B,)), _stream()))
+    dev, B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    _check(load().spcfg_preference_backward(*inputs, _here(grad_loss, "grad_loss", (n,), _F32, dev),
+                                            _here(grad_logZ, "grad_logZ", (B,), _F32, dev), _raw_stream(dev)))
 
 
 def spcfg_preference_forward_backward(logZ, ref_logZ, chosen, rejected, beta, smoothing, grad_loss, loss, margin,
                                       grad_logZ):
     """Loss, margin and gradient in one call."""
-    B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
+    dev, B, n, inputs = _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing)
     _check(load().spcfg_preference_forward_backward(
-        *inputs, _here(grad_loss, "grad_loss", (n,)), _here(loss, "loss", (n,)), _here(margin, "margin", (n,)),
-        _here(grad_logZ, "grad_logZ", (B,)), _stream()))
+        *inputs, _here(grad_loss, "grad_loss", (n,), _F32, dev), _here(loss, "loss", (n,), _F32, dev),
+        _here(margin, "margin", (n,), _F32, dev), _here(grad_logZ, "grad_logZ", (B,), _F32, dev), _raw_stream(dev)))
 
 
 def spcfg_span_marginals(cfg, lengths, n_max, workspace, span_post, span_label=None):

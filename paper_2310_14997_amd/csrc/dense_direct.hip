@@ -25,6 +25,7 @@ template <> struct Pieces<float> {
   __device__ __forceinline__ void set(const float (&v)[8]) {
     s.cut(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]));
   }
+  __device__ __forceinline__ void raw(const float (&v)[8]) { set(v); }
 };
 template <> struct Pieces<uint16_t> {
   uintx4 h;
@@ -32,6 +33,7 @@ template <> struct Pieces<uint16_t> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) h[i] = Split3::pack_rne(v[2 * i], v[2 * i + 1]);
   }
+  __device__ __forceinline__ void raw(const uint16_t (&v)[8]) { __builtin_memcpy(&h, v, 16); }
 };
 __device__ __forceinline__ floatx16 mma(uintx4 a, uintx4 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -101,62 +103,65 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
 #pragma unroll
   for (int j = 0; j < NT; ++j) rb[j] = min(n0 + 32 * j + fr, N - 1);
 
+  // U chunks at a time: everything of theirs is asked for before any of it is used
+  using T1 = typename std::conditional<FORM == FWD, TI, TO>::type;
+  constexpr int U = FORM == FWD ? 4 : 2;
   const int64_t chunks = (K + 15) / 16;
-  for (int64_t c = wave; c < chunks; c += kWaves) {
-    const int64_t k = c * 16 + fh * 8;
-    Pieces<TI> A[MT], B[NT];
-    if constexpr (FORM == FWD) {
-      TI va[MT][8], vb[NT][8];
+  for (int64_t c0 = wave; c0 < chunks; c0 += kWaves * U) {
+    T1 va[U][MT][8], vz[U][MT][8];
+    TI vb[U][NT][8];
 #pragma unroll
-      for (int i = 0; i < MT; ++i) along<TI, VEC>(x + ra[i] * g.I, k, K, va[i]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) along<TI, VEC>(W + rb[j] * g.I, k, K, vb[j]);
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = (c0 + kWaves * u) * 16 + fh * 8;  // (from K on everything is zero)
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        if constexpr (std::is_same<TI, float>::value) A[i].set(va[i]);
-        else __builtin_memcpy(&A[i].h, va[i], 16);
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if constexpr (std::is_same<TI, float>::value) B[j].set(vb[j]);
-        else __builtin_memcpy(&B[j].h, vb[j], 16);
-      }
-    } else {
-      TO vg[MT][8], vz[MT][8];
-      TI vb[NT][8];
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        if constexpr (FORM == DX) {
-          along<TO, VEC>(gy + ra[i] * g.O, k, K, vg[i]);
-          if (slope) along<TO, VEC>(z + ra[i] * g.O, k, K, vz[i]);
+        if constexpr (FORM == FWD) {
+          along<TI, VEC>(x + ra[i] * g.I, k, K, va[u][i]);
+        } else if constexpr (FORM == DX) {
+          along<TO, VEC>(gy + ra[i] * g.O, k, K, va[u][i]);
+          if (slope) along<TO, VEC>(z + ra[i] * g.O, k, K, vz[u][i]);
         } else {
-          across<TO>(gy, g.O, ra[i], k, K, vg[i]);
-          if (slope) across<TO>(z, g.O, ra[i], k, K, vz[i]);
+          across<TO>(gy, g.O, ra[i], k, K, va[u][i]);
+          if (slope) across<TO>(z, g.O, ra[i], k, K, vz[u][i]);
         }
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) across<TI>(FORM == DX ? W : x, g.I, rb[j], k, K, vb[j]);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        float d[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          d[u] = to_float<TO>(vg[i][u]);
-          if (slope) d[u] *= act_slope(g.act, to_float<TO>(vz[i][u]));
-          if (FORM == DW) bsum[i] += d[u];
-        }
-        A[i].set(d);
       }
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        if constexpr (std::is_same<TI, float>::value) B[j].set(vb[j]);
-        else __builtin_memcpy(&B[j].h, vb[j], 16);
+        if constexpr (FORM == FWD) along<TI, VEC>(W + rb[j] * g.I, k, K, vb[u][j]);
+        else across<TI>(FORM == DX ? W : x, g.I, rb[j], k, K, vb[u][j]);
       }
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int u = 0; u < U; ++u) {
+      if (c0 + kWaves * u >= chunks) break;
+      Pieces<TI> A[MT], B[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) product(A[i], B[j], acc[i][j]);
+      for (int i = 0; i < MT; ++i) {
+        if constexpr (FORM == FWD) {
+          A[i].raw(va[u][i]);
+        } else {
+          float d[8], zz[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[e] = to_float<TO>(va[u][i][e]);
+          if (slope) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) zz[e] = to_float<TO>(vz[u][i][e]);
+            times_slopes<8>(g.act, zz, d);
+          }
+          if (FORM == DW) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bsum[i] += d[e];
+          }
+          A[i].set(d);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) B[j].raw(vb[u][j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) product(A[i], B[j], acc[i][j]);
+    }
   }
 
   // the eight partial tiles, summed in the order of the wavefronts; thread t then owns whole columns of rows

@@ -6,12 +6,12 @@
 //    no activation: dz is grad_y).
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
-//    32 values of k: rows of 64 bytes along k, with the 16-byte piece XORed with bits 2..3 of the row; across k 32 rows of
-//    128 columns, with the 64-byte piece XORed with the row mod 4.  Operands come out of LDS with ds_read_b128, resp. with the
-//    transposing ds_read_b64_tr_b16; both forms meet no bank conflict.
-//  * The order of a step is written out: products of the step's first 16 k while its second 16 are read, then products of
-//    those; behind their first the barrier - each wavefront's loads of the next step have landed, nobody needs this step's
-//    tiles any more - then the next step's first operands are read and its place is filled with the tiles of step + NS.
+//    32 or 64 values of k: rows of 64 or 128 bytes along k, with the 16-byte piece XORed with bits 2..3, resp. 1..3 of the
+//    row; across k rows of 128 columns, with the 64-byte piece XORed with the row mod 4.  Operands come out of LDS with
+//    ds_read_b128, resp. with the transposing ds_read_b64_tr_b16; both forms meet no bank conflict.
+//  * The order of a step is written out: products of 16 k while the next 16 are read; behind the first products of the last 16
+//    the barrier - each wavefront's loads of the next step have landed, nobody needs this step's tiles any more - then the
+//    next step's first operands are read and this step's place is filled with the tiles of step + NS.
 //  * Few tiles: k is split over workgroups, which leave fp32 partial tiles; k_dense_join adds them in order.
 // No launch waits for another workgroup; sums run in an order fixed by the sizes.
 #include <type_traits>
@@ -29,8 +29,6 @@ using nt::lds_address;
 using nt::static_for;
 
 typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
-
-constexpr int BK = 32;  // values of k of a step
 
 // What lies beyond the end of k reads as zero.
 __device__ uintx4 g_zeros;
@@ -55,17 +53,20 @@ __device__ __forceinline__ bf16x8 operand(const uintx4& f) { return __builtin_bi
 __device__ __forceinline__ void tie(Frag& f) { asm volatile("" : "+v"(f.lo), "+v"(f.hi)); }
 __device__ __forceinline__ void tie(uintx4& f) { asm volatile("" : "+v"(f)); }
 
-// PL planes; a tile of BM x BN by WM x WN wavefronts; NS steps in LDS; TA / TB: the operand runs across k
-template <int PL_, int BM_, int BN_, int WM_, int WN_, int NS_> struct Shape {
-  static constexpr int PL = PL_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
+// PL planes; a tile of BM x BN by WM x WN wavefronts; BK values of k a step; NS steps in LDS
+template <int PL_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct Shape {
+  static constexpr int PL = PL_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
   static constexpr int NW = WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN);
-  static constexpr int PTA = BM * 64, PTB = BN * 64;  // bytes of one plane's tile
+  static constexpr int RB = 2 * BK;                   // bytes of a row along k
+  static constexpr int PTA = BM * RB, PTB = BN * RB;  // bytes of one plane's tile
   static constexpr int STAGE = PL * (PTA + PTB);
-  static constexpr int ND = PL * (BM + BN) / 16 / NW;  // 1 KB loads of a wavefront and step
-  static constexpr int NM = (PL == 3 ? 6 : 1) * MI * NI;
+  static constexpr int LA = PTA / 1024, LB = PTB / 1024;  // 1 KB loads of a plane's tile
+  static constexpr int NDA = PL * LA / NW, ND = PL * (LA + LB) / NW;  // of a wavefront and step, the first NDA of A
+  static constexpr int CH = BK / 16;                  // chunks of 16 k in a step
+  static constexpr int NM = (PL == 3 ? 6 : 1) * MI * NI;  // matrix instructions of a chunk
   static constexpr int kLds = NS * STAGE;
-  static constexpr int NDA = PL * BM / 16 / NW;          // the first of them of A
-  static_assert((BM / 16) % NW == 0 && (BN / 16) % NW == 0, "loads of a plane's tile are dealt evenly");
+  static_assert(LA % NW == 0 && LB % NW == 0, "loads of a plane's tile are dealt evenly");
+  static_assert((BK == 32 || BK == 64) && NS >= 2 && ND * (NS - 1) < 64, "");
 };
 
 #define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
@@ -97,7 +98,7 @@ __device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_
 
 template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
 __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW / 4 : S::NW / 4) k_dense_tile(Args g, Product p) {
-  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS;
+  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, BK = S::BK, CH = S::CH;
   __shared__ __align__(1024) unsigned char lds[S::kLds];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -139,24 +140,28 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   const int64_t m0 = (int64_t)tile_m * S::BM, n0 = (int64_t)tile_n * S::BN;
   const int k0 = split * p.steps_per_split, k1 = min(p.steps, k0 + p.steps_per_split);
 
-  // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 bytes; across: 4 of 256.
+  // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 or 8 of 128 bytes; across: 4
+  // of 256, BK rows of 128 columns after the other.
   // Addresses are a base per operand and plane, the same for all lanes, plus 32 bits (the host checks that these do).
   const unsigned lds0 = lds_address(lds);
   unsigned e_off[ND], e_lds[ND];
-  const int r_al = lane >> 2, c_al = (lane & 3) ^ ((lane >> 4) & 3);  // row of the 16, and piece: XOR with bits 2..3 of the row
+  constexpr int RL = 1024 / S::RB, QA = BK / 4;  // rows of a load along k; loads of 128 columns across k
+  // row of those, and piece: XOR with bits of the row (the loads of a plane are RL rows apart, a multiple of 8)
+  const int r_al = lane / (64 / RL), c_al = (lane & (64 / RL - 1)) ^ (BK == 32 ? (r_al >> 2) & 3 : 0);
   const int r_ac = lane >> 4, c_ac = (((lane & 15) >> 2) ^ r_ac) * 32 + (lane & 3) * 8;
   static_for<0, ND>([&](auto j) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
-    constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
+    constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
     const int q = wave + e0 % per;
     e_lds[jv] = (unsigned)((isA ? plane * S::PTA : PL * S::PTA + plane * S::PTB) + q * 1024);
     const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
     if constexpr (isA ? TA : TB) {
-      const int64_t col = min(o0 + (q >> 3) * 128 + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
-      e_off[jv] = (unsigned)(2 * ((4 * (q & 7) + r_ac) * ld + col));
+      const int64_t col = min(o0 + q / QA * 128 + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
+      e_off[jv] = (unsigned)(2 * ((4 * (q % QA) + r_ac) * ld + col));
     } else {
-      e_off[jv] = (unsigned)(2 * (min(o0 + 16 * q + r_al, len - 1) - o0) * ld + 16 * c_al);
+      const int piece = BK == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7);
+      e_off[jv] = (unsigned)(2 * (min(o0 + RL * q + r_al, len - 1) - o0) * ld + 16 * piece);
     }
   });
   const int64_t step_a = TA ? 2 * BK * p.lda : 2 * BK, step_b = TB ? 2 * BK * p.ldb : 2 * BK;  // bytes a step
@@ -174,7 +179,7 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   auto load_one = [&](auto j, unsigned stage) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
-    constexpr int plane = S::NW * (isA ? jv : jv - S::NDA) / ((isA ? S::BM : S::BN) / 16);
+    constexpr int plane = S::NW * (isA ? jv : jv - S::NDA) / (isA ? S::LA : S::LB);
     dma16(base[isA ? 0 : 1][plane] + e_off[jv], lds0 + stage + e_lds[jv]);
   };
   auto advance = [&]() {
@@ -185,14 +190,15 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
     }
   };
   // the last step of all where k ends inside it: what lies beyond reads as zero
-  const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * BK);  // k of the last step, 1 .. 32
+  const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * BK);  // k of the last step, 1 .. BK
   const int whole = last_left < BK ? p.steps - 1 : p.steps;        // steps that are whole
   auto load_last = [&](unsigned stage) {
     static_for<0, ND>([&](auto j) {
       constexpr int jv = decltype(j)::value;
       constexpr bool isA = jv < S::NDA;
-      constexpr int per = (isA ? S::BM : S::BN) / 16, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
-      const int k = (isA ? TA : TB) ? 4 * ((wave + e0 % per) & 7) + r_ac : c_al * 8;
+      constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
+      const int q = wave + e0 % per;
+      const int k = (isA ? TA : TB) ? 4 * (q % QA) + r_ac : 8 * (BK == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
       const unsigned char* at = base[isA ? 0 : 1][plane] + e_off[jv];
       dma16(k < last_left ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
     });
@@ -202,26 +208,26 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   unsigned fa[TA ? MI : 1], fb[TB ? NI : 1];
   {
     const int fr = lane & 31, fh = lane >> 5;
-    const unsigned al = (unsigned)(fr * 64 + (fh ^ ((fr >> 2) & 3)) * 16);
+    const unsigned al = (unsigned)(fr * S::RB + (fh ^ (BK == 32 ? (fr >> 2) & 3 : (fr >> 1) & 7)) * 16);
     const int li = lane & 15, lq = lane >> 4;
     const unsigned ac = (unsigned)((8 * (lq >> 1) + (li >> 2)) * 256 + 32 * (lq & 1) + 8 * (li & 3));
     if constexpr (TA) {
 #pragma unroll
       for (int f = 0; f < MI; ++f) {
         const int blk = wm * MI + f;
-        fa[f] = ac + (unsigned)((blk >> 2) * 8192 + (((blk & 3) ^ (li >> 2)) * 64));
+        fa[f] = ac + (unsigned)((blk >> 2) * (BK * 256) + (((blk & 3) ^ (li >> 2)) * 64));
       }
     } else {
-      fa[0] = al + (unsigned)(wm * MI * 2048);
+      fa[0] = al + (unsigned)(wm * MI * 32 * S::RB);
     }
     if constexpr (TB) {
 #pragma unroll
       for (int f = 0; f < NI; ++f) {
         const int blk = wn * NI + f;
-        fb[f] = PL * S::PTA + ac + (unsigned)((blk >> 2) * 8192 + (((blk & 3) ^ (li >> 2)) * 64));
+        fb[f] = PL * S::PTA + ac + (unsigned)((blk >> 2) * (BK * 256) + (((blk & 3) ^ (li >> 2)) * 64));
       }
     } else {
-      fb[0] = PL * S::PTA + al + (unsigned)(wn * NI * 2048);
+      fb[0] = PL * S::PTA + al + (unsigned)(wn * NI * 32 * S::RB);
     }
   }
   using FA = typename std::conditional<TA, Frag, uintx4>::type;
@@ -240,7 +246,7 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 4096 + 1024));
       } else {
         const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"(pl * S::PTA + f * 2048));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"(pl * S::PTA + f * 32 * S::RB));
       }
     } else {
       constexpr int pl = (rv - PL * MI) / NI, f = (rv - PL * MI) % NI;
@@ -250,7 +256,7 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 4096 + 1024));
       } else {
         const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"(pl * S::PTB + f * 2048));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"(pl * S::PTB + f * 32 * S::RB));
       }
     }
   };
@@ -278,9 +284,6 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
     constexpr int pb = PL == 1 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
     acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(F.a[pa][mi]), operand(F.b[pb][ni]), acc[mi][ni], 0, 0, 0);
   };
-  using C0 = std::integral_constant<int, 0>;
-  using C1 = std::integral_constant<int, 1>;
-
   const int n = k1 - k0;
   static_for<0, NS>([&](auto s) {
     constexpr int sv = decltype(s)::value;
@@ -294,26 +297,31 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   SPCFG_SB
-  if (n > 0) static_for<0, NF>([&](auto r) { read_one(X, r, 0u, C0{}); });
+  if (n > 0) static_for<0, NF>([&](auto r) { read_one(X, r, 0u, std::integral_constant<int, 0>{}); });
   unsigned cur = 0;
   constexpr int RPF = (NF + NM - 1) / NM;                          // reads behind each product of the first half
   constexpr int NB = NM >= 8 ? 2 : 1, RS = NM - NB;                // products ahead of the barrier, and behind it
   constexpr int RPS = RS > 0 ? (NF + RS - 1) / RS : NF;
   for (int i = 0; i < n; ++i) {
     const unsigned nxt = cur + S::STAGE == NS * S::STAGE ? 0 : cur + S::STAGE;
-    SPCFG_SB
-    wait_reads(X);
-    SPCFG_SB
-    static_for<0, NM>([&](auto m) {
-      constexpr int mv = decltype(m)::value;
-      mfma_one(X, m);
+    static_for<0, CH - 1>([&](auto c) {
+      constexpr int cv = decltype(c)::value;
+      Chunk &F = cv % 2 ? Y : X, &G = cv % 2 ? X : Y;
       SPCFG_SB
-      static_for<0, RPF>([&](auto q) {
-        constexpr int r = mv * RPF + decltype(q)::value;
-        if constexpr (r < NF) read_one(Y, std::integral_constant<int, r>{}, cur, C1{});
+      wait_reads(F);
+      SPCFG_SB
+      static_for<0, NM>([&](auto m) {
+        constexpr int mv = decltype(m)::value;
+        mfma_one(F, m);
+        SPCFG_SB
+        static_for<0, RPF>([&](auto q) {
+          constexpr int r = mv * RPF + decltype(q)::value;
+          if constexpr (r < NF) read_one(G, std::integral_constant<int, r>{}, cur, std::integral_constant<int, cv + 1>{});
+        });
+        SPCFG_SB
       });
-      SPCFG_SB
     });
+    SPCFG_SB
     wait_reads(Y);
     SPCFG_SB
     static_for<0, NB>([&](auto m) { mfma_one(Y, m); });
@@ -331,7 +339,7 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
       SPCFG_SB
       static_for<0, RPS>([&](auto q) {
         constexpr int r = s * RPS + decltype(q)::value;
-        if constexpr (r < NF) read_one(X, std::integral_constant<int, r>{}, nxt, C0{});
+        if constexpr (r < NF) read_one(X, std::integral_constant<int, r>{}, nxt, std::integral_constant<int, 0>{});
       });
       if (more) {
         static_for<0, ND>([&](auto j) {
@@ -469,18 +477,23 @@ __global__ void __launch_bounds__(256) k_dense_dz(Args g, uint16_t* __restrict__
   const bool vec = ((((uintptr_t)gy) | ((uintptr_t)z) | (uintptr_t)(g.O * sizeof(TO))) & 15) == 0;
   float s[8] = {};
   if (c < ld) {
-    for (int64_t r = (int64_t)part * span + wave; r < r1; r += 4) {
-      float d[8];
-      eight<TO>(gy, g.R, g.O, r, c, vec, d);
+    // (four rows' loads in flight)
+    for (int64_t r0 = (int64_t)part * span + wave; r0 < r1; r0 += 16) {
+      float d[4][8], y[4][8];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) eight<TO>(gy, g.R, g.O, r0 + 4 * u, c, vec, d[u]);
       if (g.act != SPCFG_ACT_NONE) {
-        float y[8];
-        eight<TO>(z, g.R, g.O, r, c, vec, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] *= act_slope(g.act, y[i]);
+        for (int u = 0; u < 4; ++u) eight<TO>(z, g.R, g.O, r0 + 4 * u, c, vec, y[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) times_slopes<8>(g.act, y[u], d[u]);
       }
-      if (dst) put_planes(dst + r * ld + c, rows32 * ld, d, TI());
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += d[i];
+      for (int u = 0; u < 4; ++u) {
+        if (dst && r0 + 4 * u < r1) put_planes(dst + (r0 + 4 * u) * ld + c, rows32 * ld, d[u], TI());
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += d[u][i];
+      }
     }
   }
   if (!sums) return;
@@ -497,25 +510,18 @@ __global__ void __launch_bounds__(256) k_dense_dz(Args g, uint16_t* __restrict__
 }
 
 // ---- which form, and what it needs -----------------------------------------------------------------------------------------
-struct Form { int bm, bn, tiles_m, tiles_n, steps, splits, per; };
+struct Form { bool wide; int splits; };
 
-// splits: enough workgroups for all CUs, of at least 8 steps each
+// wide: tiles of 256 x 256; splits: enough workgroups for all CUs, of at least 256 k each
 Form form_of(int64_t M, int64_t N, int64_t K, bool fp32) {
-  Form f;
-  const int steps = (int)((K + BK - 1) / BK);
   auto tiles = [](int64_t n, int t) { return (n + t - 1) / t; };
-  f.bm = 128;
-  f.bn = 128;
-  if (!fp32 && tiles(M, 256) * tiles(N, 256) >= 256 && K >= 2048) f.bm = f.bn = 256;
-  f.tiles_m = (int)tiles(M, f.bm);
-  f.tiles_n = (int)tiles(N, f.bn);
-  f.steps = steps;
-  const int64_t t = (int64_t)f.tiles_m * f.tiles_n, room = fp32 ? 256 : 512;
-  int64_t sp = t >= room / 2 ? 1 : room / t;
-  if (sp > steps / 8) sp = steps / 8;
-  if (sp < 1) sp = 1;
-  f.per = (int)((steps + sp - 1) / sp);
-  f.splits = (steps + f.per - 1) / f.per;
+  Form f;
+  f.wide = !fp32 && tiles(M, 256) * tiles(N, 256) >= 256 && K >= 2048;
+  const int t = f.wide ? 256 : 128;
+  const int64_t all = tiles(M, t) * tiles(N, t), room = fp32 ? 256 : 512;
+  int64_t sp = all >= room / 2 ? 1 : room / all;
+  if (sp > K / 256) sp = K / 256;
+  f.splits = (int)(sp < 1 ? 1 : sp);
   return f;
 }
 
@@ -547,8 +553,8 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   p.w = up32(O) * up32(I);
   p.z = up32(R) * up32(O);
   const int64_t cb = (up32(O) + 511) / 512;
-  int64_t span = (up32(R) * cb / 1024 + 31) / 32 * 32;
-  if (span < 32) span = 32;
+  int64_t span = (up32(R) * cb / 1024 + 15) / 16 * 16;  // about 1024 workgroups, 16 rows at a time
+  if (span < 16) span = 16;
   p.span = (int)span;
   p.parts = (int)((up32(R) + span - 1) / span);
   p.fwd = form_of(R, O, I, fp32);
@@ -573,28 +579,29 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   return p;
 }
 
-template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
-void launch(const Args& a, const Product& p, hipStream_t st) {
-  hipLaunchKernelGGL((k_dense_tile<S, TA, TB, TI, TO, FORM>), dim3(p.tiles_m * p.tiles_n * p.splits + p.bias_blocks), dim3(64 * S::NW), 0, st, a, p);
-}
-
-template <typename TI, typename TO, int FORM>
-void product(const Args& a, Product p, const Form& f, hipStream_t st) {
+// Grid and steps follow from the shape that is launched, so that the two cannot disagree; splits only go down from the plan's.
+template <typename S, typename TI, typename TO, int FORM>
+void launch(const Args& a, Product p, int splits, hipStream_t st) {
   constexpr bool TA = FORM == DW, TB = FORM != FWD;
-  p.steps = f.steps;
-  p.steps_per_split = f.per;
-  p.splits = f.splits;
-  p.tiles_m = f.tiles_m;
-  p.tiles_n = f.tiles_n;
-  if constexpr (std::is_same<TI, float>::value) {
-    launch<Shape<3, 128, 128, 2, 2, 3>, TA, TB, TI, TO, FORM>(a, p, st);
-  } else {
-    if (f.bm == 256) launch<Shape<1, 256, 256, 2, 2, 4>, TA, TB, TI, TO, FORM>(a, p, st);
-    else launch<Shape<1, 128, 128, 2, 2, 4>, TA, TB, TI, TO, FORM>(a, p, st);
-  }
+  p.tiles_m = (unsigned)((p.M + S::BM - 1) / S::BM);
+  p.tiles_n = (unsigned)((p.N + S::BN - 1) / S::BN);
+  p.steps = (int)((p.K + S::BK - 1) / S::BK);
+  p.steps_per_split = (p.steps + splits - 1) / splits;
+  p.splits = (p.steps + p.steps_per_split - 1) / p.steps_per_split;
+  hipLaunchKernelGGL((k_dense_tile<S, TA, TB, TI, TO, FORM>), dim3(p.tiles_m * p.tiles_n * p.splits + p.bias_blocks), dim3(64 * S::NW), 0, st, a, p);
   if (p.splits > 1) {
     const int64_t blocks = (p.M * ((p.N + 7) / 8) + 255) / 256;
     hipLaunchKernelGGL((k_dense_join<TI, TO, FORM>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a, p);
+  }
+}
+
+template <typename TI, typename TO, int FORM>
+void product(const Args& a, const Product& p, const Form& f, hipStream_t st) {
+  if constexpr (std::is_same<TI, float>::value) {
+    launch<Shape<3, 128, 128, 2, 2, 32, 3>, TI, TO, FORM>(a, p, f.splits, st);
+  } else {
+    if (f.wide) launch<Shape<1, 256, 256, 2, 4, 64, 2>, TI, TO, FORM>(a, p, f.splits, st);
+    else launch<Shape<1, 128, 128, 2, 2, 64, 2>, TI, TO, FORM>(a, p, f.splits, st);
   }
 }
 

@@ -109,7 +109,7 @@ template <typename T> struct Row {
 
 // ---- the teacher's entries ---------------------------------------------------------------------------------------------
 struct Entries {
-  int id[kMostEntries];     // -1 where absent
+  alignas(16) int id[kMostEntries];  // -1 where absent, and up to the next multiple of 4
   float p[kMostEntries];
 };
 struct Teacher {
@@ -132,6 +132,7 @@ __device__ Teacher teacher_row(const Args& g, int64_t row, Entries& E, float* re
     E.p[e] = a;
     if (id >= 0) top = fmaxf(top, a);
   }
+  if (threadIdx.x < 3 && g.k + threadIdx.x < (unsigned)((g.k + 3) / 4 * 4)) E.id[g.k + threadIdx.x] = -1;
   top = all_max<NT>(top, red);
   wrong = all_max<NT>(wrong, red);
   float total = 0.0f;
@@ -178,15 +179,28 @@ __device__ void write_entries(const Args& g, int64_t row, const Entries& E, floa
   T* o = static_cast<T*>(g.grad) + row * g.V;
   for (int e = threadIdx.x; e < g.k; e += NT) {
     const int id = E.id[e];
-    if (id < 0 || id < lo || id >= hi) continue;
-    float p = 0.0f;
-    bool first = true;
-    for (int f = 0; f < g.k; ++f) {
-      if (E.id[f] != id) continue;
-      if (f < e) { first = false; break; }
-      p += E.p[f];
+    const bool mine = id >= 0 && id >= lo && id < hi;
+    if (!__any(mine)) continue;
+    const float q = mine ? q_of(id) : 0.0f;
+    // equal ids: any before this one, any behind it (four at a time; from k on there is no id)
+    bool before = false, behind = false;
+#pragma unroll 4
+    for (int f = 0; f < g.k; f += 4) {
+      const int4 at = *reinterpret_cast<const int4*>(&E.id[f]);
+      const int v[4] = {at.x, at.y, at.z, at.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        before |= v[u] == id && f + u < e;
+        behind |= v[u] == id && f + u > e;
+      }
     }
-    if (first) o[id] = from_float<T>(scale * (q_of(id) - p));
+    if (!mine || before) continue;
+    float p = E.p[e];
+    if (behind) {
+      for (int f = e + 1; f < g.k; ++f)
+        if (E.id[f] == id) p += E.p[f];
+    }
+    o[id] = from_float<T>(scale * (q - p));
   }
 }
 

@@ -3,10 +3,12 @@
 //   margin = (logZ_c - ref_c) - (logZ_r - ref_r),   x = beta margin
 //   loss   = (1 - eps) softplus(-x) + eps softplus(x)
 //   d loss / d margin = beta (eps s(x) - (1 - eps) s(-x)),  s(x) = 1 / (1 + exp(-x)); + at c, - at r
-// One launch: workgroups of the first kind take the pairs, those of the second kind sentences, a wavefront for each four:
-// it looks through all pairs, 64 at a time, and adds the ones that its sentences are part of.  No atomics: a sentence
-// in many pairs has its sum in a fixed order (lane by lane, then across lanes), in 64 bits, as are the differences of log
-// Z, which are small beside log Z itself.  Bound by latency at the sizes of a batch.
+// One launch: workgroups of the first kind take the pairs, those of the second kind four sentences each.  These look through
+// all pairs, a segment of 1024 per wavefront at a time with every load in flight, list the ones that their sentences are part
+// of in LDS (in order), and then take the list 64 pairs at a time: what it takes to work a pair out, and its latency, is spent on
+// the few pairs that matter.  No atomics: a sentence in many pairs has its sum in a fixed order (lane by lane, across lanes,
+// across wavefronts), in 64 bits, as are the differences of log Z, which are small beside log Z itself.  Bound by latency at
+// the sizes of a batch.
 #include <cmath>
 
 #include "spcfg_internal.h"
@@ -14,7 +16,8 @@
 namespace spcfg {
 namespace {
 
-constexpr int kOwn = 4;        // sentences of a wavefront
+constexpr int kOwn = 4;        // sentences of a workgroup
+constexpr int kSeg = 16;       // pairs a lane looks through at a time
 constexpr int kMostPairs = 1 << 20, kMostSentences = 1 << 16;
 
 struct Args {
@@ -48,6 +51,8 @@ __device__ __forceinline__ float weight_of(const Args& g, float margin) {
 }
 
 __global__ void __launch_bounds__(256) k_preference(Args g, int pair_blocks) {
+  __shared__ int list[4][kSeg * 64];
+  __shared__ double red[4][kOwn];
   if ((int)blockIdx.x < pair_blocks) {
     const int p = blockIdx.x * 256 + threadIdx.x;
     if (p >= g.n) return;
@@ -61,29 +66,48 @@ __global__ void __launch_bounds__(256) k_preference(Args g, int pair_blocks) {
     g.margin[p] = m;
     return;
   }
-  const int lane = threadIdx.x & 63;
-  const int s0 = (((int)blockIdx.x - pair_blocks) * 4 + (int)(threadIdx.x >> 6)) * kOwn;
-  if (s0 >= g.B) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int s0 = ((int)blockIdx.x - pair_blocks) * kOwn;
   double acc[kOwn] = {};
-  for (int p = lane; p < g.n; p += 64) {
-    const int i = g.chosen[p], j = g.rejected[p];
-    if ((i < s0 || i >= s0 + kOwn) && (j < s0 || j >= s0 + kOwn)) continue;
-    bool out;
-    const float m = margin_of(g, i, j, &out);
-    if (out || i == j) continue;  // (a sentence against itself adds and takes away the same)
-    const double w = (double)weight_of(g, m) * (g.grad_loss ? g.grad_loss[p] : 1.0f);
+  for (int seg = wave * kSeg * 64; seg < g.n; seg += 4 * kSeg * 64) {
+    int i[kSeg], j[kSeg], found = 0;
 #pragma unroll
-    for (int u = 0; u < kOwn; ++u) {
-      if (i == s0 + u) acc[u] += w;
-      if (j == s0 + u) acc[u] -= w;
+    for (int u = 0; u < kSeg; ++u) {
+      const int p = seg + u * 64 + lane;
+      i[u] = p < g.n ? g.chosen[p] : -1;
+      j[u] = p < g.n ? g.rejected[p] : -1;
     }
+#pragma unroll
+    for (int u = 0; u < kSeg; ++u) {
+      const bool mine = (unsigned)(i[u] - s0) < (unsigned)kOwn || (unsigned)(j[u] - s0) < (unsigned)kOwn;
+      const unsigned long long m = __ballot(mine);
+      if (mine) list[wave][found + __popcll(m & ((1ull << lane) - 1))] = seg + u * 64 + lane;
+      found += __popcll(m);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wavefront reads only what it listed itself)
+    for (int h = lane; h < found; h += 64) {
+      const int p = list[wave][h], c = g.chosen[p], r = g.rejected[p];
+      bool out;
+      const float m = margin_of(g, c, r, &out);
+      if (out || c == r) continue;  // (a sentence against itself adds and takes away the same)
+      const double w = (double)weight_of(g, m) * (g.grad_loss ? g.grad_loss[p] : 1.0f);
+#pragma unroll
+      for (int u = 0; u < kOwn; ++u) {
+        if (c == s0 + u) acc[u] += w;
+        if (r == s0 + u) acc[u] -= w;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 #pragma unroll
   for (int u = 0; u < kOwn; ++u) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc[u] += __shfl_xor(acc[u], o, 64);
-    if (lane == 0 && s0 + u < g.B) g.grad[s0 + u] = (float)acc[u];
+    if (lane == 0) red[wave][u] = acc[u];
   }
+  __syncthreads();
+  const int u = threadIdx.x;
+  if (u < kOwn && s0 + u < g.B) g.grad[s0 + u] = (float)(((red[0][u] + red[1][u]) + red[2][u]) + red[3][u]);
 }
 
 int run(int32_t B, int32_t n, const float* logZ, const float* ref, const int32_t* chosen, const int32_t* rejected, float beta,
@@ -100,7 +124,7 @@ int run(int32_t B, int32_t n, const float* logZ, const float* ref, const int32_t
       const uintptr_t a = (uintptr_t)at[o].p, b = (uintptr_t)at[i].p;
       if (o != i && a && b && a < b + 4 * at[i].len && b < a + 4 * at[o].len) return SPCFG_ERR_ARG;
     }
-  const int pb = forward ? (n + 255) / 256 : 0, sb = backward ? (B + 4 * kOwn - 1) / (4 * kOwn) : 0;
+  const int pb = forward ? (n + 255) / 256 : 0, sb = backward ? (B + kOwn - 1) / kOwn : 0;
   if (pb + sb == 0) return SPCFG_OK;
   const Args a{B, n, logZ, ref, chosen, rejected, beta, eps, grad_loss, loss, margin, grad};
   hipLaunchKernelGGL(k_preference, dim3(pb + sb), dim3(256), 0, st, a, pb);
