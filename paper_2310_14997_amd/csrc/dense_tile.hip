@@ -1,8 +1,8 @@
 // Dense layers, large products: C[m][n] = sum_k A(m,k) B(n,k) on tiles in LDS, operands as bf16 planes.
 //
 //  * bf16 operands are one plane, read where they lie; fp32 operands are cut exactly into three (nt::Split3: hi, mid, lo) by
-//    k_dense_cut and multiplied as six piece products, accumulated in fp32; dz = grad_y * act'(z) is written as one or
-//    three planes by k_dense_dz, which adds up the bias's gradient on the way (not needed where grad_y is bf16 and there is
+//    k_dense_prepare and multiplied as six piece products, accumulated in fp32; dz = grad_y * act'(z) is written as one or
+//    three planes by the same kernel, which adds up the bias's gradient on the way (not needed where grad_y is bf16 and there is
 //    no activation: dz is grad_y).
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
@@ -12,7 +12,7 @@
 //  * The order of a step is written out: products of 16 k while the next 16 are read; behind the first products of the last 16
 //    the barrier - each wavefront's loads of the next step have landed, nobody needs this step's tiles any more - then the
 //    next step's first operands are read and this step's place is filled with the tiles of step + NS.
-//  * Few tiles: k is split over workgroups, which leave fp32 partial tiles; k_dense_join adds them in order.
+//  * Few tiles: k is split over workgroups, which leave fp32 partial tiles; a second launch adds them in order.
 // No launch waits for another workgroup; sums run in an order fixed by the sizes.
 #include <type_traits>
 #include <utility>
@@ -38,10 +38,8 @@ struct Product {
   int64_t lda, ldb, plane_a, plane_b;  // in elements
   int64_t M, N, K;                     // K: rows, resp. columns that may be read along k
   int steps, steps_per_split, splits;
-  unsigned tiles_m, tiles_n;
+  unsigned tiles_m, tiles_n, wgs;
   float* partial;                      // [splits][M][N] where splits > 1
-  const float* bias_part;              // dW: [bias_parts][O] sums of dz over parts of the rows
-  int bias_parts, bias_blocks;
 };
 
 // One operand of one plane: eight k of a row or column per lane.
@@ -96,40 +94,18 @@ __device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_
   }
 }
 
-template <typename S, bool TA, bool TB, typename TI, typename TO, int FORM>
-__global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW / 4 : S::NW / 4) k_dense_tile(Args g, Product p) {
+// One tile of one product: workgroup `b` of `all`, both counted from a multiple of 8.
+template <typename S, typename TI, typename TO, int FORM>
+__device__ __forceinline__ void tile_product(const Args& g, const Product& p, unsigned b, unsigned all, unsigned char* lds) {
+  constexpr bool TA = FORM == DW, TB = FORM != FWD;
   constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, BK = S::BK, CH = S::CH;
-  __shared__ __align__(1024) unsigned char lds[S::kLds];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % S::WM, wn = wave / S::WM;
 
-  if (FORM == DW && (int)blockIdx.x < p.bias_blocks) {
-    // the bias's gradient: 64 columns a workgroup, the parts dealt to the wavefronts, joined in their order
-    float* red = reinterpret_cast<float*>(lds);
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (c < p.M) {
-#pragma unroll 4
-      for (int q = wave; q < p.bias_parts; q += S::NW) s += p.bias_part[(int64_t)q * p.M + c];
-    }
-    red[wave * 64 + lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < p.M) {
-#pragma unroll
-      for (int w = 1; w < S::NW; ++w) s += red[w * 64 + lane];
-      store_bias<TI>(g, c, s);
-    }
-    return;
-  }
-
   // which tile: each XCD takes a run of consecutive ones, which form blocks of up to 8 row tiles
-  unsigned t;
-  {
-    const unsigned b = blockIdx.x - (FORM == DW ? p.bias_blocks : 0), n = gridDim.x - (FORM == DW ? p.bias_blocks : 0);
-    const unsigned xcd = b & 7, q = n >> 3, r = n & 7;
-    t = xcd * q + min(xcd, r) + (b >> 3);
-  }
+  const unsigned xcd = b & 7;
+  unsigned t = xcd * (all >> 3) + min(xcd, all & 7) + (b >> 3);
   const unsigned per_split = p.tiles_m * p.tiles_n;
   const int split = __builtin_amdgcn_readfirstlane(t / per_split);
   t -= split * per_split;
@@ -388,13 +364,57 @@ __global__ void __launch_bounds__(64 * S::NW, S::kLds <= 80 * 1024 ? 2 * S::NW /
   });
 }
 
+// The bias's gradient: 64 columns a workgroup, the parts of the rows dealt to the wavefronts, joined in their order.
+template <int NW, typename TI>
+__device__ __forceinline__ void bias_sums(const Args& g, const float* __restrict__ part, int parts, unsigned block, float* red) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)block * 64 + lane;
+  float s = 0.0f;
+  if (c < g.O) {
+#pragma unroll 4
+    for (int q = wave; q < parts; q += NW) s += part[(int64_t)q * g.O + c];
+  }
+  red[wave * 64 + lane] = s;
+  __syncthreads();
+  if (wave == 0 && c < g.O) {
+#pragma unroll
+    for (int w = 1; w < NW; ++w) s += red[w * 64 + lane];
+    store_bias<TI>(g, c, s);
+  }
+}
+
+// 2 wavefronts per SIMD or more; two workgroups per CU where LDS has room for them
+template <typename S> constexpr int waves_per_simd() { return S::kLds <= 80 * 1024 ? 2 * S::NW / 4 : S::NW / 4; }
+
+template <typename S, typename TI, typename TO>
+__global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>()) k_dense_forward_tiles(Args g, Product p) {
+  __shared__ __align__(1024) unsigned char lds[S::kLds];
+  tile_product<S, TI, TO, FWD>(g, p, blockIdx.x, p.wgs, lds);
+}
+
+// Both products of the backward pass and the bias's gradient in one launch: the CUs that one leaves idle are the other's.  Each
+// part's workgroups start at a multiple of 8, so that the XCD is the same function of either index.
+template <typename S, typename TI, typename TO>
+__global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>()) k_dense_backward_tiles(Args g, Product px, Product pw, const float* sums, int parts) {
+  __shared__ __align__(1024) unsigned char lds[S::kLds];
+  unsigned b = blockIdx.x;
+  const unsigned room_x = (px.wgs + 7) / 8 * 8, room_w = (pw.wgs + 7) / 8 * 8;
+  if (b < room_x) {
+    if (b < px.wgs) tile_product<S, TI, TO, DX>(g, px, b, px.wgs, lds);
+  } else if ((b -= room_x) < room_w) {
+    if (b < pw.wgs) tile_product<S, TI, TO, DW>(g, pw, b, pw.wgs, lds);
+  } else {
+    bias_sums<S::NW, TI>(g, sums, parts, b - room_w, reinterpret_cast<float*>(lds));
+  }
+}
+
 // Partial tiles added up in the order of their k, eight columns a thread.
 template <typename TI, typename TO, int FORM>
-__global__ void __launch_bounds__(256) k_dense_join(Args g, Product p) {
+__device__ __forceinline__ void join(const Args& g, const Product& p, unsigned block, unsigned blocks) {
   const int64_t per_row = (p.N + 7) / 8, n = p.M * per_row, all = p.M * p.N;
   const Epilogue<TI, TO, FORM> ep(g, p.N);
   const bool vec = (p.N & 3) == 0;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
+  for (int64_t e = (int64_t)block * 256 + threadIdx.x; e < n; e += (int64_t)blocks * 256) {
     const int64_t m = e / per_row, c = (e - m * per_row) * 8;
     float s[8] = {}, bias[8];
 #pragma unroll 4
@@ -405,16 +425,19 @@ __global__ void __launch_bounds__(256) k_dense_join(Args g, Product p) {
   }
 }
 
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) k_dense_forward_join(Args g, Product p) {
+  join<TI, TO, FWD>(g, p, blockIdx.x, gridDim.x);
+}
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) k_dense_backward_join(Args g, Product px, Product pw, unsigned blocks_x) {
+  if (blockIdx.x < blocks_x) join<TI, TO, DX>(g, px, blockIdx.x, blocks_x);
+  else join<TI, TO, DW>(g, pw, blockIdx.x - blocks_x, gridDim.x - blocks_x);
+}
+
 // ---- planes --------------------------------------------------------------------------------------------------------------
 // Rows and columns of a matrix in planes are rounded up to a step's 32, with zeros, so that products may run along either.
 int64_t up32(int64_t n) { return (n + 31) / 32 * 32; }
-
-struct Cut {
-  const void* src[2];
-  uint16_t* dst[2];
-  int64_t rows[2], cols[2];
-  unsigned blocks0;  // workgroups of the first matrix
-};
 
 __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t plane, const float (&v)[8], float) {
   Split3 s;
@@ -447,29 +470,33 @@ __device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, i
   for (int i = 0; i < 8; ++i) v[i] = to_float<T>(x[i]);
 }
 
-// The planes of one or two matrices.  Bound by HBM: fp32 10 bytes a value.
+// Planes of one matrix, eight values a thread.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dense_cut(Cut c) {
-  const int w = blockIdx.x >= c.blocks0;
-  const T* src = static_cast<const T*>(c.src[w]);
-  const int64_t rows = c.rows[w], cols = c.cols[w], ld = (cols + 31) / 32 * 32, rows32 = (rows + 31) / 32 * 32;
-  const int64_t e = ((int64_t)(blockIdx.x - (w ? c.blocks0 : 0)) * 256 + threadIdx.x) * 8;
+__device__ __forceinline__ void cut(const T* __restrict__ src, uint16_t* __restrict__ dst, int64_t rows, int64_t cols, unsigned block) {
+  const int64_t ld = (cols + 31) / 32 * 32, rows32 = (rows + 31) / 32 * 32, e = ((int64_t)block * 256 + threadIdx.x) * 8;
   if (e >= rows32 * ld) return;
-  const int64_t r = e / ld, col = e % ld;
+  int64_t r, c;
+  if (e < ((int64_t)1 << 31)) {  // (a division in 32 bits is far cheaper)
+    r = (unsigned)e / (unsigned)ld;
+    c = (unsigned)e - (unsigned)r * (unsigned)ld;
+  } else {
+    r = e / ld;
+    c = e - r * ld;
+  }
   const bool vec = ((((uintptr_t)src) | (uintptr_t)(cols * sizeof(T))) & 15) == 0;
   float v[8];
-  eight<T>(src, rows, cols, r, col, vec, v);
-  put_planes(c.dst[w] + e, rows32 * ld, v, T());
+  eight<T>(src, rows, cols, r, c, vec, v);
+  put_planes(dst + e, rows32 * ld, v, T());
 }
 
 // dz = grad_y * act'(z) in planes (where dst is given) and, part by part of the rows, its sums over them (where sums is): 512
 // columns and `span` rows a workgroup, a row per wavefront at a time.
 template <typename TI, typename TO>
-__global__ void __launch_bounds__(256) k_dense_dz(Args g, uint16_t* __restrict__ dst, float* __restrict__ sums, int span, unsigned col_blocks) {
-  __shared__ float red[3][512];
+__device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ dst, float* __restrict__ sums, int span,
+                                        unsigned col_blocks, unsigned block, float (*red)[512]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)(blockIdx.x % col_blocks) * 512 + lane * 8;
-  const unsigned part = blockIdx.x / col_blocks;
+  const int64_t c = (int64_t)(block % col_blocks) * 512 + lane * 8;
+  const unsigned part = block / col_blocks;
   const int64_t ld = (g.O + 31) / 32 * 32, rows32 = (g.R + 31) / 32 * 32;
   const int64_t r1 = min(rows32, (int64_t)(part + 1) * span);
   const TO* gy = static_cast<const TO*>(g.grad_y);
@@ -509,20 +536,47 @@ __global__ void __launch_bounds__(256) k_dense_dz(Args g, uint16_t* __restrict__
   }
 }
 
-// ---- which form, and what it needs -----------------------------------------------------------------------------------------
-struct Form { bool wide; int splits; };
+// What a product reads that is not there yet, in one launch: dz and the sums for the bias's gradient, planes of x, planes of W.
+// Bound by HBM: 10 bytes a value of fp32 operands.
+struct Prepare {
+  uint16_t *dz, *x, *W;
+  float* sums;
+  int span;
+  unsigned col_blocks, blocks_z, blocks_x;  // workgroups of each, W's the rest
+};
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) k_dense_prepare(Args g, Prepare q) {
+  __shared__ float red[3][512];
+  unsigned b = blockIdx.x;
+  if (b < q.blocks_z) make_dz<TI, TO>(g, q.dz, q.sums, q.span, q.col_blocks, b, red);
+  else if ((b -= q.blocks_z) < q.blocks_x) cut<TI>(static_cast<const TI*>(g.x), q.x, g.R, g.I, b);
+  else cut<TI>(static_cast<const TI*>(g.W), q.W, g.O, g.I, b - q.blocks_x);
+}
 
-// wide: tiles of 256 x 256; splits: enough workgroups for all CUs, of at least 256 k each
-Form form_of(int64_t M, int64_t N, int64_t K, bool fp32) {
-  auto tiles = [](int64_t n, int t) { return (n + t - 1) / t; };
-  Form f;
-  f.wide = !fp32 && tiles(M, 256) * tiles(N, 256) >= 256 && K >= 2048;
-  const int t = f.wide ? 256 : 128;
-  const int64_t all = tiles(M, t) * tiles(N, t), room = fp32 ? 256 : 512;
-  int64_t sp = all >= room / 2 ? 1 : room / all;
-  if (sp > K / 256) sp = K / 256;
-  f.splits = (int)(sp < 1 ? 1 : sp);
-  return f;
+// ---- which form, and what it needs -----------------------------------------------------------------------------------------
+int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
+
+// A product as tiles of t x t that go through all of k: `n` of them, of `steps` steps.
+struct Work { int64_t n, steps; };
+Work work_of(int64_t M, int64_t N, int64_t K, int t, int bk) { return Work{tiles(M, t) * tiles(N, t), tiles(K, bk)}; }
+
+// Into how many workgroups each tile's steps are cut, for two products of one launch (or one, b.n = 0).  `room` workgroups run at a
+// time; what the launch takes is estimated as the longest share where all of them run at once, as the mean with half a share
+// on top where they do not, plus, per split, `join` steps for writing and adding its partial tiles.  Of the share lengths
+// that cut the longer product into 1, 2, 3, ... the best is taken; a share has at least `least` steps.
+void choose_splits(Work a, Work b, int64_t room, int64_t least, double join, int* sa, int* sb) {
+  double best = 1e30;
+  const int64_t longer = b.n && b.steps > a.steps ? b.steps : a.steps;
+  for (int64_t s = 1; s <= 32 && (s == 1 || longer / s >= least); ++s) {
+    const int64_t len = tiles(longer, (int)s), pa = tiles(a.steps, (int)len), pb = b.n ? tiles(b.steps, (int)len) : 0;
+    const int64_t la = tiles(a.steps, (int)pa), lb = pb ? tiles(b.steps, (int)pb) : 0, wgs = a.n * pa + b.n * pb;
+    const double most = (double)(la > lb ? la : lb), mean = (double)(a.n * pa * la + b.n * pb * lb) / room;
+    double t = wgs <= room ? most : mean + 0.5 * most;
+    if (t < most) t = most;
+    const int64_t parts = (pa > 1 ? a.n * pa : 0) + (pb > 1 ? b.n * pb : 0);
+    if (parts) t += 4 + join * parts / room;
+    if (t < best) { best = t; *sa = (int)pa; *sb = (int)(pb ? pb : 1); }
+  }
 }
 
 bool large(int64_t R, int64_t I, int64_t O) {
@@ -532,13 +586,15 @@ bool large(int64_t R, int64_t I, int64_t O) {
 
 struct Plan {
   bool on;                 // whether the layer takes tiled products at all
+  bool wide;               // tiles of 256 x 256 (all products of the call)
   bool cut;                // x and W as planes (fp32, or rows that do not lie on 16 bytes)
   bool dz;                 // dz as planes
   int pl;
   int64_t x, w, z;         // elements of one plane of x, W, dz
   int span, parts;         // rows of a part of the bias's gradient
-  Form fwd, dx, dw;
-  size_t off_x, off_w, off_z, off_sums, off_part, bytes;
+  int fwd, dx, dw;         // splits; dx1, dw1 where the other product of the backward pass is not wanted
+  int dx1, dw1;
+  size_t off_x, off_w, off_z, off_sums, off_px, off_pw, bytes;
 };
 
 Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
@@ -552,82 +608,98 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   p.x = up32(R) * up32(I);
   p.w = up32(O) * up32(I);
   p.z = up32(R) * up32(O);
-  const int64_t cb = (up32(O) + 511) / 512;
+  const int64_t cb = tiles(up32(O), 512);
   int64_t span = (up32(R) * cb / 1024 + 15) / 16 * 16;  // about 1024 workgroups, 16 rows at a time
   if (span < 16) span = 16;
   p.span = (int)span;
-  p.parts = (int)((up32(R) + span - 1) / span);
-  p.fwd = form_of(R, O, I, fp32);
-  p.dx = form_of(R, I, O, fp32);
-  p.dw = form_of(O, I, R, fp32);
+  p.parts = (int)tiles(up32(R), p.span);
+  // wide tiles: a CU's worth of them for every CU and sums long enough to make up for their longer start and end
+  // (8192 x 4096 x 4096: 241 us, 320 on 128 x 128; 2048 x 512 x 10000: 61 us, 43)
+  p.wide = !fp32 && tiles(R, 256) * tiles(O, 256) >= 256 && I >= 2048;
+  const int t = p.wide ? 256 : 128, bk = fp32 ? 32 : 64;
+  const int64_t room = fp32 || p.wide ? 256 : 512, least = fp32 ? 6 : 3;
+  const double join = fp32 ? 4 : 8;
+  int none;
+  const Work wf = work_of(R, O, I, t, bk), wx = work_of(R, I, O, t, bk), ww = work_of(O, I, R, t, bk), w0{0, 0};
+  choose_splits(wf, w0, room, least, join, &p.fwd, &none);
+  choose_splits(wx, ww, room, least, join, &p.dx, &p.dw);
+  choose_splits(wx, w0, room, least, join, &p.dx1, &none);
+  choose_splits(ww, w0, room, least, join, &p.dw1, &none);
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
+  auto partial = [&](int splits, int more, int64_t M, int64_t N) {
+    const int s = splits > more ? splits : more;
+    return s > 1 ? (size_t)s * M * N * 4 : 0;
+  };
   p.off_x = take(p.cut ? (size_t)p.x * 2 * p.pl : 0);
   p.off_w = take(p.cut ? (size_t)p.w * 2 * p.pl : 0);
+  const size_t forward_part = at;
   p.off_z = take(p.dz ? (size_t)p.z * 2 * p.pl : 0);
   p.off_sums = take((size_t)p.parts * O * 4);
-  size_t part = 0;
-  auto partial = [&](const Form& f, int64_t M, int64_t N) {
-    const size_t n = f.splits > 1 ? (size_t)f.splits * M * N * 4 : 0;
-    if (n > part) part = n;
-  };
-  partial(p.fwd, R, O);
-  partial(p.dx, R, I);
-  partial(p.dw, O, I);
-  p.off_part = take(part);
-  p.bytes = at;
+  p.off_px = take(partial(p.dx, p.dx1, R, I));
+  p.off_pw = take(partial(p.dw, p.dw1, O, I));
+  // the forward product's partial tiles lie where the backward pass keeps dz and its own
+  const size_t fwd_end = forward_part + partial(p.fwd, 1, R, O);
+  p.bytes = at > fwd_end ? at : (fwd_end + 255) / 256 * 256;
   return p;
 }
 
 // Grid and steps follow from the shape that is launched, so that the two cannot disagree; splits only go down from the plan's.
-template <typename S, typename TI, typename TO, int FORM>
-void launch(const Args& a, Product p, int splits, hipStream_t st) {
-  constexpr bool TA = FORM == DW, TB = FORM != FWD;
-  p.tiles_m = (unsigned)((p.M + S::BM - 1) / S::BM);
-  p.tiles_n = (unsigned)((p.N + S::BN - 1) / S::BN);
-  p.steps = (int)((p.K + S::BK - 1) / S::BK);
-  p.steps_per_split = (p.steps + splits - 1) / splits;
-  p.splits = (p.steps + p.steps_per_split - 1) / p.steps_per_split;
-  hipLaunchKernelGGL((k_dense_tile<S, TA, TB, TI, TO, FORM>), dim3(p.tiles_m * p.tiles_n * p.splits + p.bias_blocks), dim3(64 * S::NW), 0, st, a, p);
-  if (p.splits > 1) {
-    const int64_t blocks = (p.M * ((p.N + 7) / 8) + 255) / 256;
-    hipLaunchKernelGGL((k_dense_join<TI, TO, FORM>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a, p);
-  }
+template <typename S> void shape_up(Product* p, int splits) {
+  p->tiles_m = (unsigned)tiles(p->M, S::BM);
+  p->tiles_n = (unsigned)tiles(p->N, S::BN);
+  p->steps = (int)tiles(p->K, S::BK);
+  p->steps_per_split = (int)tiles(p->steps, splits);
+  p->splits = (int)tiles(p->steps, p->steps_per_split);
+  p->wgs = p->tiles_m * p->tiles_n * p->splits;
+}
+unsigned join_blocks(const Product& p) {
+  const int64_t n = p.splits > 1 ? tiles(p.M * tiles(p.N, 8), 256) : 0;
+  return (unsigned)(n < 4096 ? n : 4096);
 }
 
-template <typename TI, typename TO, int FORM>
-void product(const Args& a, const Product& p, const Form& f, hipStream_t st) {
-  if constexpr (std::is_same<TI, float>::value) {
-    launch<Shape<3, 128, 128, 2, 2, 32, 3>, TI, TO, FORM>(a, p, f.splits, st);
-  } else {
-    if (f.wide) launch<Shape<1, 256, 256, 2, 4, 64, 2>, TI, TO, FORM>(a, p, f.splits, st);
-    else launch<Shape<1, 128, 128, 2, 2, 64, 2>, TI, TO, FORM>(a, p, f.splits, st);
-  }
+template <typename S, typename TI, typename TO>
+void launch_forward(const Args& a, Product p, int splits, hipStream_t st) {
+  shape_up<S>(&p, splits);
+  hipLaunchKernelGGL((k_dense_forward_tiles<S, TI, TO>), dim3(p.wgs), dim3(64 * S::NW), 0, st, a, p);
+  if (p.splits > 1) hipLaunchKernelGGL((k_dense_forward_join<TI, TO>), dim3(join_blocks(p)), dim3(256), 0, st, a, p);
+}
+template <typename S, typename TI, typename TO>
+void launch_backward(const Args& a, Product x, Product w, int sx, int sw, const float* sums, int parts, hipStream_t st) {
+  if (a.grad_x) shape_up<S>(&x, sx);
+  if (a.grad_W) shape_up<S>(&w, sw);
+  const unsigned n = (x.wgs + 7) / 8 * 8 + (w.wgs + 7) / 8 * 8 + (sums ? (unsigned)tiles(a.O, 64) : 0);
+  hipLaunchKernelGGL((k_dense_backward_tiles<S, TI, TO>), dim3(n), dim3(64 * S::NW), 0, st, a, x, w, sums, parts);
+  const unsigned jx = join_blocks(x), jw = join_blocks(w);
+  if (jx + jw) hipLaunchKernelGGL((k_dense_backward_join<TI, TO>), dim3(jx + jw), dim3(256), 0, st, a, x, w, jx);
 }
 
-template <typename T> void cut(const void* x, uint16_t* px, int64_t R, const void* W, uint16_t* pw, int64_t O, int64_t I, hipStream_t st) {
-  auto blocks = [&](int64_t rows) { return (unsigned)((up32(rows) * up32(I) / 8 + 255) / 256); };
-  const unsigned b0 = x ? blocks(R) : 0, b1 = W ? blocks(O) : 0;
-  Cut c{{x, W}, {px, pw}, {R, O}, {I, I}, b0};
-  hipLaunchKernelGGL(k_dense_cut<T>, dim3(b0 + b1), dim3(256), 0, st, c);
-}
+// The shapes: two wavefronts per SIMD, one issuing while the other waits
+using Fp32 = Shape<3, 128, 128, 2, 4, 32, 3>;
+using Bf16 = Shape<1, 128, 128, 2, 4, 64, 2>;
+using Bf16Wide = Shape<1, 256, 256, 2, 4, 64, 2>;
 
 template <typename TI, typename TO>
 void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   Product q{};
   q.M = a.R;
   q.N = a.O;
-  q.partial = reinterpret_cast<float*>(ws + p.off_part);
+  q.partial = reinterpret_cast<float*>(ws + p.off_z);
   if (p.cut) {
-    uint16_t *px = reinterpret_cast<uint16_t*>(ws + p.off_x), *pw = reinterpret_cast<uint16_t*>(ws + p.off_w);
-    cut<TI>(a.x, px, a.R, a.W, pw, a.O, a.I, st);
-    q.A = px; q.B = pw; q.plane_a = p.x; q.plane_b = p.w;
+    Prepare r{};
+    r.x = reinterpret_cast<uint16_t*>(ws + p.off_x);
+    r.W = reinterpret_cast<uint16_t*>(ws + p.off_w);
+    r.blocks_x = (unsigned)tiles(p.x / 8, 256);
+    hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(r.blocks_x + (unsigned)tiles(p.w / 8, 256)), dim3(256), 0, st, a, r);
+    q.A = r.x; q.B = r.W; q.plane_a = p.x; q.plane_b = p.w;
     q.lda = q.ldb = q.K = up32(a.I);
   } else {
     q.A = static_cast<const uint16_t*>(a.x); q.B = static_cast<const uint16_t*>(a.W);
     q.lda = q.ldb = q.K = a.I;
   }
-  product<TI, TO, FWD>(a, q, p.fwd, st);
+  if constexpr (std::is_same<TI, float>::value) launch_forward<Fp32, TI, TO>(a, q, p.fwd, st);
+  else if (p.wide) launch_forward<Bf16Wide, TI, TO>(a, q, p.fwd, st);
+  else launch_forward<Bf16, TI, TO>(a, q, p.fwd, st);
 }
 
 template <typename TI, typename TO>
@@ -635,38 +707,40 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   const uint16_t *x = static_cast<const uint16_t*>(a.x), *W = static_cast<const uint16_t*>(a.W);
   const uint16_t* z = static_cast<const uint16_t*>(a.grad_y);
   int64_t ldi = a.I, ldo = a.O;
-  bool kx = false, kz = false;  // whether rows are padded with zeros to a whole step
+  Prepare r{};
+  unsigned blocks_w = 0;
   if (p.cut) {
-    uint16_t *px = reinterpret_cast<uint16_t*>(ws + p.off_x), *pw = reinterpret_cast<uint16_t*>(ws + p.off_w);
-    cut<TI>(a.grad_W ? a.x : nullptr, px, a.R, a.grad_x ? a.W : nullptr, pw, a.O, a.I, st);
-    x = px; W = pw; ldi = up32(a.I); kx = true;
+    r.x = reinterpret_cast<uint16_t*>(ws + p.off_x);
+    r.W = reinterpret_cast<uint16_t*>(ws + p.off_w);
+    if (a.grad_W) r.blocks_x = (unsigned)tiles(p.x / 8, 256);
+    if (a.grad_x) blocks_w = (unsigned)tiles(p.w / 8, 256);
+    x = r.x; W = r.W; ldi = up32(a.I);
   }
-  float* sums = a.grad_bias ? reinterpret_cast<float*>(ws + p.off_sums) : nullptr;
-  uint16_t* pz = p.dz ? reinterpret_cast<uint16_t*>(ws + p.off_z) : nullptr;
-  if (pz || sums) {
-    const unsigned cb = (unsigned)((up32(a.O) + 511) / 512);
-    hipLaunchKernelGGL((k_dense_dz<TI, TO>), dim3(cb * p.parts), dim3(256), 0, st, a, pz, sums, p.span, cb);
+  if (a.grad_bias) r.sums = reinterpret_cast<float*>(ws + p.off_sums);
+  if (p.dz) { r.dz = reinterpret_cast<uint16_t*>(ws + p.off_z); z = r.dz; ldo = up32(a.O); }
+  if (r.dz || r.sums) {
+    r.span = p.span;
+    r.col_blocks = (unsigned)tiles(up32(a.O), 512);
+    r.blocks_z = r.col_blocks * p.parts;
   }
-  if (pz) { z = pz; ldo = up32(a.O); kz = true; }
-  Product q{};
-  q.partial = reinterpret_cast<float*>(ws + p.off_part);
-  if (a.grad_x) {
-    q.A = z; q.lda = ldo; q.plane_a = p.z;
-    q.B = W; q.ldb = ldi; q.plane_b = p.w;
-    q.M = a.R; q.N = a.I;
-    q.K = kz && kx ? up32(a.O) : a.O;
-    product<TI, TO, DX>(a, q, p.dx, st);
-  }
-  if (a.grad_W) {
-    q.A = z; q.lda = ldo; q.plane_a = p.z;
-    q.B = x; q.ldb = ldi; q.plane_b = p.x;
-    q.M = a.O; q.N = a.I;
-    q.K = kz && kx ? up32(a.R) : a.R;
-    q.bias_part = sums;
-    q.bias_parts = p.parts;
-    q.bias_blocks = sums ? (int)((a.O + 63) / 64) : 0;
-    product<TI, TO, DW>(a, q, p.dw, st);
-  }
+  const unsigned n = r.blocks_z + r.blocks_x + blocks_w;
+  if (n) hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(n), dim3(256), 0, st, a, r);
+  const bool padded = p.cut && p.dz;  // whether the rows of both operands go on, as zeros, to a multiple of 32
+  Product dx{}, dw{};
+  dx.A = z; dx.lda = ldo; dx.plane_a = p.z;
+  dx.B = W; dx.ldb = ldi; dx.plane_b = p.w;
+  dx.M = a.R; dx.N = a.I;
+  dx.K = padded ? up32(a.O) : a.O;
+  dx.partial = reinterpret_cast<float*>(ws + p.off_px);
+  dw.A = z; dw.lda = ldo; dw.plane_a = p.z;
+  dw.B = x; dw.ldb = ldi; dw.plane_b = p.x;
+  dw.M = a.O; dw.N = a.I;
+  dw.K = padded ? up32(a.R) : a.R;
+  dw.partial = reinterpret_cast<float*>(ws + p.off_pw);
+  const int sx = a.grad_W ? p.dx : p.dx1, sw = a.grad_x ? p.dw : p.dw1;
+  if constexpr (std::is_same<TI, float>::value) launch_backward<Fp32, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
+  else if (p.wide) launch_backward<Bf16Wide, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
+  else launch_backward<Bf16, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
 }
 
 }  // namespace
