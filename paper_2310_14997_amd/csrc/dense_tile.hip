@@ -1,9 +1,15 @@
-// Dense layers, large products: C[m][n] = sum_k A(m,k) B(n,k) on tiles in LDS, operands as bf16 planes.
+// Dense layers, large products: C[m][n] = sum_k A(m,k) B(n,k) on tiles in LDS, operands as planes of 16-bit values.
 //
-//  * bf16 operands are one plane, read where they lie; fp32 operands are cut exactly into three (nt::Split3: hi, mid, lo) by
-//    k_dense_prepare and multiplied as six piece products, accumulated in fp32; dz = grad_y * act'(z) is written as one or
-//    three planes by the same kernel, which adds up the bias's gradient on the way (not needed where grad_y is bf16 and there is
-//    no activation: dz is grad_y).
+//  * bf16 operands are one plane, read where they lie.
+//  * fp32 operands of the forward product are two fp16 planes: a row is scaled by a power of two so that its largest value lies
+//    in [2^14, 2^15), hi = fp16(v), lo = fp16(2^11 (v - hi)), and C = sum hi hi + 2^-11 sum (hi lo + lo hi), the two sums in
+//    fp32 accumulators of their own.  hi + 2^-11 lo is v to 2^-23 (for values down to 2^-29 of their row's largest; below that to
+//    2^-51 of it) and the dropped lo lo is at most 2^-22 of a term: the accuracy of an fp32 product, whatever a row's scale, for
+//    half the matrix work of the next form.  Without the 2^11 lo would lose bits from 2^-16 of the largest value on.
+//  * fp32 operands of the backward products are cut exactly into three bf16 planes (nt::Split3: hi, mid, lo) and multiplied as
+//    six piece products: these run across rows, whose scales could not be taken out of the sum.
+//  * dz = grad_y * act'(z) is written as one or three planes by the kernel that cuts, which adds up the bias's gradient on the
+//    way (not needed where grad_y is bf16 and there is no activation: dz is grad_y).
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
 //    32 or 64 values of k: rows of 64 or 128 bytes along k, with the 16-byte piece XORed with bits 2..3, resp. 1..3 of the
@@ -29,6 +35,7 @@ using nt::lds_address;
 using nt::static_for;
 
 typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
 // What lies beyond the end of k reads as zero.
 __device__ uintx4 g_zeros;
@@ -40,6 +47,7 @@ struct Product {
   int steps, steps_per_split, splits;
   unsigned tiles_m, tiles_n, wgs;
   float* partial;                      // [splits][M][N] where splits > 1
+  const int *exp_a, *exp_b;            // fp16 planes: powers of two that the rows of A and B are scaled by
 };
 
 // One operand of one plane: eight k of a row or column per lane.
@@ -51,20 +59,24 @@ __device__ __forceinline__ bf16x8 operand(const uintx4& f) { return __builtin_bi
 __device__ __forceinline__ void tie(Frag& f) { asm volatile("" : "+v"(f.lo), "+v"(f.hi)); }
 __device__ __forceinline__ void tie(uintx4& f) { asm volatile("" : "+v"(f)); }
 
-// PL planes; a tile of BM x BN by WM x WN wavefronts; BK values of k a step; NS steps in LDS
+// PL planes; a tile of BM x BN by WM x WN wavefronts; BK values of k a step; NS steps in LDS.  Two planes lie side by side, 32
+// values of one and the same 32 of the other, so that a step is a whole line of 128 bytes of each row: to loads they are
+// MP = 1 plane of ME = 64 values a step.
 template <int PL_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct Shape {
   static constexpr int PL = PL_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
   static constexpr int NW = WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN);
-  static constexpr int RB = 2 * BK;                   // bytes of a row along k
+  static constexpr int MP = PL == 2 ? 1 : PL, ME = PL == 2 ? 2 * BK : BK;
+  static constexpr int RB = 2 * ME;                   // bytes of a row along k
   static constexpr int PTA = BM * RB, PTB = BN * RB;  // bytes of one plane's tile
-  static constexpr int STAGE = PL * (PTA + PTB);
+  static constexpr int STAGE = MP * (PTA + PTB);
   static constexpr int LA = PTA / 1024, LB = PTB / 1024;  // 1 KB loads of a plane's tile
-  static constexpr int NDA = PL * LA / NW, ND = PL * (LA + LB) / NW;  // of a wavefront and step, the first NDA of A
+  static constexpr int NDA = MP * LA / NW, ND = MP * (LA + LB) / NW;  // of a wavefront and step, the first NDA of A
   static constexpr int CH = BK / 16;                  // chunks of 16 k in a step
-  static constexpr int NM = (PL == 3 ? 6 : 1) * MI * NI;  // matrix instructions of a chunk
+  static constexpr int NM = (PL == 3 ? 6 : PL == 2 ? 3 : 1) * MI * NI;  // matrix instructions of a chunk
+  static constexpr int NA = PL == 2 ? 2 : 1;          // sums: fp16 planes keep the small products apart
   static constexpr int kLds = NS * STAGE;
   static_assert(LA % NW == 0 && LB % NW == 0, "loads of a plane's tile are dealt evenly");
-  static_assert((BK == 32 || BK == 64) && NS >= 2 && ND * (NS - 1) < 64, "");
+  static_assert((ME == 32 || ME == 64) && (PL != 2 || BK == 32) && NS >= 2 && ND * (NS - 1) < 64, "");
 };
 
 #define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
@@ -98,7 +110,8 @@ __device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_
 template <typename S, typename TI, typename TO, int FORM>
 __device__ __forceinline__ void tile_product(const Args& g, const Product& p, unsigned b, unsigned all, unsigned char* lds) {
   constexpr bool TA = FORM == DW, TB = FORM != FWD;
-  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, BK = S::BK, CH = S::CH;
+  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, CH = S::CH, MP = S::MP, ME = S::ME;
+  static_assert(PL != 2 || FORM == FWD, "two planes run along k");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % S::WM, wn = wave / S::WM;
@@ -117,32 +130,32 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   const int k0 = split * p.steps_per_split, k1 = min(p.steps, k0 + p.steps_per_split);
 
   // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 or 8 of 128 bytes; across: 4
-  // of 256, BK rows of 128 columns after the other.
+  // of 256, ME rows of 128 columns after the other.
   // Addresses are a base per operand and plane, the same for all lanes, plus 32 bits (the host checks that these do).
   const unsigned lds0 = lds_address(lds);
   unsigned e_off[ND], e_lds[ND];
-  constexpr int RL = 1024 / S::RB, QA = BK / 4;  // rows of a load along k; loads of 128 columns across k
+  constexpr int RL = 1024 / S::RB, QA = ME / 4;  // rows of a load along k; loads of 128 columns across k
   // row of those, and piece: XOR with bits of the row (the loads of a plane are RL rows apart, a multiple of 8)
-  const int r_al = lane / (64 / RL), c_al = (lane & (64 / RL - 1)) ^ (BK == 32 ? (r_al >> 2) & 3 : 0);
+  const int r_al = lane / (64 / RL), c_al = (lane & (64 / RL - 1)) ^ (ME == 32 ? (r_al >> 2) & 3 : 0);
   const int r_ac = lane >> 4, c_ac = (((lane & 15) >> 2) ^ r_ac) * 32 + (lane & 3) * 8;
   static_for<0, ND>([&](auto j) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
     constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
     const int q = wave + e0 % per;
-    e_lds[jv] = (unsigned)((isA ? plane * S::PTA : PL * S::PTA + plane * S::PTB) + q * 1024);
+    e_lds[jv] = (unsigned)((isA ? plane * S::PTA : MP * S::PTA + plane * S::PTB) + q * 1024);
     const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
     if constexpr (isA ? TA : TB) {
       const int64_t col = min(o0 + q / QA * 128 + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
       e_off[jv] = (unsigned)(2 * ((4 * (q % QA) + r_ac) * ld + col));
     } else {
-      const int piece = BK == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7);
+      const int piece = ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7);
       e_off[jv] = (unsigned)(2 * (min(o0 + RL * q + r_al, len - 1) - o0) * ld + 16 * piece);
     }
   });
-  const int64_t step_a = TA ? 2 * BK * p.lda : 2 * BK, step_b = TB ? 2 * BK * p.ldb : 2 * BK;  // bytes a step
-  const unsigned char* base[2][PL];  // of the step that is loaded next
-  static_for<0, PL>([&](auto pl) {
+  const int64_t step_a = TA ? 2 * ME * p.lda : 2 * ME, step_b = TB ? 2 * ME * p.ldb : 2 * ME;  // bytes a step
+  const unsigned char* base[2][MP];  // of the step that is loaded next
+  static_for<0, MP>([&](auto pl) {
     constexpr int v = decltype(pl)::value;
     base[0][v] = reinterpret_cast<const unsigned char*>(p.A + v * p.plane_a + (TA ? m0 : m0 * p.lda)) + k0 * step_a;
     base[1][v] = reinterpret_cast<const unsigned char*>(p.B + v * p.plane_b + (TB ? n0 : n0 * p.ldb)) + k0 * step_b;
@@ -160,21 +173,21 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   };
   auto advance = [&]() {
 #pragma unroll
-    for (int v = 0; v < PL; ++v) {
+    for (int v = 0; v < MP; ++v) {
       base[0][v] += by_a;
       base[1][v] += by_b;
     }
   };
   // the last step of all where k ends inside it: what lies beyond reads as zero
-  const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * BK);  // k of the last step, 1 .. BK
-  const int whole = last_left < BK ? p.steps - 1 : p.steps;        // steps that are whole
+  const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * ME);  // values of the last step, 1 .. ME
+  const int whole = last_left < ME ? p.steps - 1 : p.steps;        // steps that are whole
   auto load_last = [&](unsigned stage) {
     static_for<0, ND>([&](auto j) {
       constexpr int jv = decltype(j)::value;
       constexpr bool isA = jv < S::NDA;
       constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
       const int q = wave + e0 % per;
-      const int k = (isA ? TA : TB) ? 4 * (q % QA) + r_ac : 8 * (BK == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
+      const int k = (isA ? TA : TB) ? 4 * (q % QA) + r_ac : 8 * (ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
       const unsigned char* at = base[isA ? 0 : 1][plane] + e_off[jv];
       dma16(k < last_left ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
     });
@@ -184,14 +197,14 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   unsigned fa[TA ? MI : 1], fb[TB ? NI : 1];
   {
     const int fr = lane & 31, fh = lane >> 5;
-    const unsigned al = (unsigned)(fr * S::RB + (fh ^ (BK == 32 ? (fr >> 2) & 3 : (fr >> 1) & 7)) * 16);
+    const unsigned al = (unsigned)(fr * S::RB + (fh ^ (ME == 32 ? (fr >> 2) & 3 : (fr >> 1) & 7)) * 16);
     const int li = lane & 15, lq = lane >> 4;
     const unsigned ac = (unsigned)((8 * (lq >> 1) + (li >> 2)) * 256 + 32 * (lq & 1) + 8 * (li & 3));
     if constexpr (TA) {
 #pragma unroll
       for (int f = 0; f < MI; ++f) {
         const int blk = wm * MI + f;
-        fa[f] = ac + (unsigned)((blk >> 2) * (BK * 256) + (((blk & 3) ^ (li >> 2)) * 64));
+        fa[f] = ac + (unsigned)((blk >> 2) * (ME * 256) + (((blk & 3) ^ (li >> 2)) * 64));
       }
     } else {
       fa[0] = al + (unsigned)(wm * MI * 32 * S::RB);
@@ -200,10 +213,10 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 #pragma unroll
       for (int f = 0; f < NI; ++f) {
         const int blk = wn * NI + f;
-        fb[f] = PL * S::PTA + ac + (unsigned)((blk >> 2) * (BK * 256) + (((blk & 3) ^ (li >> 2)) * 64));
+        fb[f] = MP * S::PTA + ac + (unsigned)((blk >> 2) * (ME * 256) + (((blk & 3) ^ (li >> 2)) * 64));
       }
     } else {
-      fb[0] = PL * S::PTA + al + (unsigned)(wn * NI * 32 * S::RB);
+      fb[0] = MP * S::PTA + al + (unsigned)(wn * NI * 32 * S::RB);
     }
   }
   using FA = typename std::conditional<TA, Frag, uintx4>::type;
@@ -221,8 +234,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].lo) : "v"(at), "n"(pl * S::PTA + cv * 4096));
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 4096 + 1024));
       } else {
-        const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"(pl * S::PTA + f * 32 * S::RB));
+        const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTA) + f * 32 * S::RB));
       }
     } else {
       constexpr int pl = (rv - PL * MI) / NI, f = (rv - PL * MI) % NI;
@@ -231,8 +244,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].lo) : "v"(at), "n"(pl * S::PTB + cv * 4096));
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 4096 + 1024));
       } else {
-        const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"(pl * S::PTB + f * 32 * S::RB));
+        const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTB) + f * 32 * S::RB));
       }
     }
   };
@@ -246,20 +259,28 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       for (int f = 0; f < NI; ++f) tie(F.b[pl][f]);
     }
   };
-  floatx16 acc[MI][NI];
+  floatx16 acc[S::NA][MI][NI];
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+  for (int a = 0; a < S::NA; ++a)
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[a][i][j][v] = 0.0f;
   auto mfma_one = [&](Chunk& F, auto i) {
-    // three planes: lo*hi, hi*lo, mid*mid, mid*hi, hi*mid, hi*hi (0 hi, 1 mid, 2 lo)
     constexpr int pp = decltype(i)::value / (MI * NI), rem = decltype(i)::value % (MI * NI), mi = rem / NI, ni = rem % NI;
-    constexpr int pa = PL == 1 ? 0 : pp == 0 ? 2 : (pp == 2 || pp == 3 ? 1 : 0);
-    constexpr int pb = PL == 1 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
-    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(F.a[pa][mi]), operand(F.b[pb][ni]), acc[mi][ni], 0, 0, 0);
+    if constexpr (PL == 2) {  // lo*hi and hi*lo into the second sum, hi*hi into the first (0 hi, 1 lo)
+      constexpr int pa = pp == 0 ? 1 : 0, pb = pp == 1 ? 1 : 0, a = pp == 2 ? 0 : 1;
+      acc[a][mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, F.a[pa][mi]),
+                                                              __builtin_bit_cast(halfx8, F.b[pb][ni]), acc[a][mi][ni], 0, 0, 0);
+    } else {  // three planes: lo*hi, hi*lo, mid*mid, mid*hi, hi*mid, hi*hi (0 hi, 1 mid, 2 lo)
+      constexpr int pa = PL == 1 ? 0 : pp == 0 ? 2 : (pp == 2 || pp == 3 ? 1 : 0);
+      constexpr int pb = PL == 1 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
+      acc[0][mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(F.a[pa][mi]), operand(F.b[pb][ni]), acc[0][mi][ni], 0, 0, 0);
+    }
   };
+
   const int n = k1 - k0;
   static_for<0, NS>([&](auto s) {
     constexpr int sv = decltype(s)::value;
@@ -342,11 +363,19 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   float bias[8];
 #pragma unroll
   for (int u = 0; u < 8; ++u) bias[u] = ep.bias_of(c + u, p.N);
+  auto total = [&](int mi, int ni, int v) {
+    return S::NA == 2 ? fmaf(acc[S::NA - 1][mi][ni][v], 0x1p-11f, acc[0][mi][ni][v]) : acc[0][mi][ni][v];
+  };
+  int down[8];
+  if (PL == 2) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) down[u] = p.exp_b[min(c + u, p.N - 1)];
+  }
   static_for<0, MI>([&](auto i) {
     constexpr int mi = decltype(i)::value;
     static_for<0, 16 * NI>([&](auto w) {
       constexpr int v = decltype(w)::value / NI, ni = decltype(w)::value % NI;
-      out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * LR + ni * 32 + (lane & 31)] = acc[mi][ni][v];
+      out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * LR + ni * 32 + (lane & 31)] = total(mi, ni, v);
     });
     // (a wavefront's own accesses to LDS are in order; the fences keep the compiler's)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -357,6 +386,11 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 #pragma unroll
       for (int u = 0; u < 8; ++u) s[u] = from[u];
       if (m >= p.M || c >= p.N) continue;
+      if (PL == 2) {
+        const int e = p.exp_a[m];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[u] = __builtin_amdgcn_ldexpf(s[u], -(e + down[u]));
+      }
       if (part) put_floats(part + m * p.N + c, s, p.N - c, (p.N & 3) == 0);
       else ep.eight(m * p.N + c, s, bias, p.N - c);
     }
@@ -553,6 +587,70 @@ __global__ void __launch_bounds__(256) k_dense_prepare(Args g, Prepare q) {
   else cut<TI>(static_cast<const TI*>(g.W), q.W, g.O, g.I, b - q.blocks_x);
 }
 
+// fp16 planes of the rows of x and W and the powers of two that they are scaled by.  A group of `group` lanes (a power of two, eight
+// values a lane at a time) takes a row: its largest magnitude, then the pieces.  Up to 32 values a lane stay in registers
+// in between, longer rows are read again.  A row of zeros, or with an infinity in it, keeps its scale.
+struct Halves {
+  const float* src[2];
+  _Float16* dst[2];
+  int* exps[2];
+  int64_t rows[2], cols;
+  unsigned blocks0;  // workgroups of the first matrix
+  int group;
+};
+__global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
+  const int w = blockIdx.x >= h.blocks0;
+  const int G = h.group, gl = threadIdx.x & (G - 1);
+  const int64_t r = (int64_t)(blockIdx.x - (w ? h.blocks0 : 0)) * (256 / G) + threadIdx.x / G;
+  if (r >= h.rows[w]) return;  // (whole groups at a time)
+  const float* src = h.src[w];
+  const int64_t cols = h.cols, ld = (cols + 31) / 32 * 32;
+  const bool vec = ((((uintptr_t)src) | (uintptr_t)(cols * 4)) & 15) == 0;
+  constexpr int E = 4;
+  float v[E][8];
+  float m = 0.0f;
+  const bool kept = ld <= (int64_t)G * 8 * E;
+  if (kept) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) eight<float>(src, h.rows[w], cols, r, ((int64_t)e * G + gl) * 8, vec, v[e]);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[e][i]));
+  } else {
+    for (int64_t c = gl * 8; c < ld; c += G * 8) {
+      eight<float>(src, h.rows[w], cols, r, c, vec, v[0]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[0][i]));
+    }
+  }
+  for (int o = 1; o < G; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const int e = m > 0.0f && m < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(m) + 1 : 0;  // (m = f 2^x with f in [1/2, 1))
+  if (gl == 0) h.exps[w][r] = e;
+  auto put = [&](int64_t c, const float (&x)[8]) {
+    if (c >= ld) return;
+    halfx8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float s = __builtin_amdgcn_ldexpf(x[i], e);
+      hi[i] = (_Float16)s;
+      lo[i] = (_Float16)((s - (float)hi[i]) * 0x1p11f);
+    }
+    _Float16* d = h.dst[w] + 2 * r * ld + c / 32 * 64 + c % 32;
+    *reinterpret_cast<halfx8*>(d) = hi;
+    *reinterpret_cast<halfx8*>(d + 32) = lo;
+  };
+  if (kept) {
+#pragma unroll
+    for (int e2 = 0; e2 < E; ++e2) put(((int64_t)e2 * G + gl) * 8, v[e2]);
+  } else {
+    for (int64_t c = gl * 8; c < ld; c += G * 8) {
+      eight<float>(src, h.rows[w], cols, r, c, vec, v[0]);
+      put(c, v[0]);
+    }
+  }
+}
+
 // ---- which form, and what it needs -----------------------------------------------------------------------------------------
 int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
 
@@ -560,11 +658,12 @@ int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
 struct Work { int64_t n, steps; };
 Work work_of(int64_t M, int64_t N, int64_t K, int t, int bk) { return Work{tiles(M, t) * tiles(N, t), tiles(K, bk)}; }
 
-// Into how many workgroups each tile's steps are cut, for two products of one launch (or one, b.n = 0).  `room` workgroups run at a
-// time; what the launch takes is estimated as the longest share where all of them run at once, as the mean with half a share
-// on top where they do not, plus, per split, `join` steps for writing and adding its partial tiles.  Of the share lengths
-// that cut the longer product into 1, 2, 3, ... the best is taken; a share has at least `least` steps.
-void choose_splits(Work a, Work b, int64_t room, int64_t least, double join, int* sa, int* sb) {
+// Into how many workgroups each tile's steps are cut, for two products of one launch (or one, b.n = 0).  What the launch takes
+// is estimated in us: `step` a step, the longest share where all of `room` workgroups run at once, the mean with half a share on
+// top where they do not; splitting costs a launch more (3 us) and partial tiles of `tile` values written and read again at
+// 4 TB/s.  Of the share lengths that cut the longer product into 1, 2, 3, ... the best is taken; a share has at least
+// `least` steps.  Measured: 4096 x 512 x 512 in fp32 (128 tiles of 16 steps) in two 37 us, in one 25.
+void choose_splits(Work a, Work b, int64_t room, int64_t least, double step, int64_t tile, int* sa, int* sb) {
   double best = 1e30;
   const int64_t longer = b.n && b.steps > a.steps ? b.steps : a.steps;
   for (int64_t s = 1; s <= 32 && (s == 1 || longer / s >= least); ++s) {
@@ -573,8 +672,9 @@ void choose_splits(Work a, Work b, int64_t room, int64_t least, double join, int
     const double most = (double)(la > lb ? la : lb), mean = (double)(a.n * pa * la + b.n * pb * lb) / room;
     double t = wgs <= room ? most : mean + 0.5 * most;
     if (t < most) t = most;
+    t *= step;
     const int64_t parts = (pa > 1 ? a.n * pa : 0) + (pb > 1 ? b.n * pb : 0);
-    if (parts) t += 4 + join * parts / room;
+    if (parts) t += 3 + 2e-6 * parts * tile;
     if (t < best) { best = t; *sa = (int)pa; *sb = (int)(pb ? pb : 1); }
   }
 }
@@ -594,7 +694,7 @@ struct Plan {
   int span, parts;         // rows of a part of the bias's gradient
   int fwd, dx, dw;         // splits; dx1, dw1 where the other product of the backward pass is not wanted
   int dx1, dw1;
-  size_t off_x, off_w, off_z, off_sums, off_px, off_pw, bytes;
+  size_t off_x, off_w, off_e, off_z, off_sums, off_px, off_pw, bytes;
 };
 
 Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
@@ -617,14 +717,15 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   // (8192 x 4096 x 4096: 241 us, 320 on 128 x 128; 2048 x 512 x 10000: 61 us, 43)
   p.wide = !fp32 && tiles(R, 256) * tiles(O, 256) >= 256 && I >= 2048;
   const int t = p.wide ? 256 : 128, bk = fp32 ? 32 : 64;
-  const int64_t room = fp32 || p.wide ? 256 : 512, least = fp32 ? 6 : 3;
-  const double join = fp32 ? 4 : 8;
+  const int64_t room_f = p.wide ? 256 : 512, room = fp32 || p.wide ? 256 : 512, least = fp32 ? 6 : 3;
+  // us a step where every CU has as many workgroups as it holds
+  const double step_f = p.wide ? 0.95 : 0.6, step = fp32 ? 1.2 : step_f;
   int none;
   const Work wf = work_of(R, O, I, t, bk), wx = work_of(R, I, O, t, bk), ww = work_of(O, I, R, t, bk), w0{0, 0};
-  choose_splits(wf, w0, room, least, join, &p.fwd, &none);
-  choose_splits(wx, ww, room, least, join, &p.dx, &p.dw);
-  choose_splits(wx, w0, room, least, join, &p.dx1, &none);
-  choose_splits(ww, w0, room, least, join, &p.dw1, &none);
+  choose_splits(wf, w0, room_f, least, step_f, t * t, &p.fwd, &none);
+  choose_splits(wx, ww, room, least, step, t * t, &p.dx, &p.dw);
+  choose_splits(wx, w0, room, least, step, t * t, &p.dx1, &none);
+  choose_splits(ww, w0, room, least, step, t * t, &p.dw1, &none);
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
   auto partial = [&](int splits, int more, int64_t M, int64_t N) {
@@ -633,6 +734,7 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   };
   p.off_x = take(p.cut ? (size_t)p.x * 2 * p.pl : 0);
   p.off_w = take(p.cut ? (size_t)p.w * 2 * p.pl : 0);
+  p.off_e = take(fp32 ? (size_t)(R + O) * 4 : 0);
   const size_t forward_part = at;
   p.off_z = take(p.dz ? (size_t)p.z * 2 * p.pl : 0);
   p.off_sums = take((size_t)p.parts * O * 4);
@@ -648,7 +750,7 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
 template <typename S> void shape_up(Product* p, int splits) {
   p->tiles_m = (unsigned)tiles(p->M, S::BM);
   p->tiles_n = (unsigned)tiles(p->N, S::BN);
-  p->steps = (int)tiles(p->K, S::BK);
+  p->steps = (int)tiles(p->K, S::ME);
   p->steps_per_split = (int)tiles(p->steps, splits);
   p->splits = (int)tiles(p->steps, p->steps_per_split);
   p->wgs = p->tiles_m * p->tiles_n * p->splits;
@@ -675,7 +777,8 @@ void launch_backward(const Args& a, Product x, Product w, int sx, int sw, const 
 }
 
 // The shapes: two wavefronts per SIMD, one issuing while the other waits
-using Fp32 = Shape<3, 128, 128, 2, 4, 32, 3>;
+using Fp32 = Shape<2, 128, 128, 2, 4, 32, 2>;      // forward
+using Fp32Back = Shape<3, 128, 128, 2, 4, 32, 3>;
 using Bf16 = Shape<1, 128, 128, 2, 4, 64, 2>;
 using Bf16Wide = Shape<1, 256, 256, 2, 4, 64, 2>;
 
@@ -685,13 +788,27 @@ void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   q.M = a.R;
   q.N = a.O;
   q.partial = reinterpret_cast<float*>(ws + p.off_z);
-  if (p.cut) {
+  if constexpr (std::is_same<TI, float>::value) {
+    Halves h{};
+    h.src[0] = static_cast<const float*>(a.x); h.src[1] = static_cast<const float*>(a.W);
+    h.dst[0] = reinterpret_cast<_Float16*>(ws + p.off_x); h.dst[1] = reinterpret_cast<_Float16*>(ws + p.off_w);
+    h.exps[0] = reinterpret_cast<int*>(ws + p.off_e); h.exps[1] = h.exps[0] + a.R;
+    h.rows[0] = a.R; h.rows[1] = a.O;
+    h.cols = a.I;
+    h.group = 8;
+    while (h.group < 64 && h.group * 8 < a.I) h.group *= 2;
+    h.blocks0 = (unsigned)tiles(a.R, 256 / h.group);
+    hipLaunchKernelGGL(k_dense_halves, dim3(h.blocks0 + (unsigned)tiles(a.O, 256 / h.group)), dim3(256), 0, st, h);
+    q.A = reinterpret_cast<const uint16_t*>(h.dst[0]); q.B = reinterpret_cast<const uint16_t*>(h.dst[1]);
+    q.exp_a = h.exps[0]; q.exp_b = h.exps[1];
+    q.lda = q.ldb = q.K = 2 * up32(a.I);
+  } else if (p.cut) {
     Prepare r{};
     r.x = reinterpret_cast<uint16_t*>(ws + p.off_x);
     r.W = reinterpret_cast<uint16_t*>(ws + p.off_w);
     r.blocks_x = (unsigned)tiles(p.x / 8, 256);
     hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(r.blocks_x + (unsigned)tiles(p.w / 8, 256)), dim3(256), 0, st, a, r);
-    q.A = r.x; q.B = r.W; q.plane_a = p.x; q.plane_b = p.w;
+    q.A = r.x; q.B = r.W;
     q.lda = q.ldb = q.K = up32(a.I);
   } else {
     q.A = static_cast<const uint16_t*>(a.x); q.B = static_cast<const uint16_t*>(a.W);
@@ -738,7 +855,7 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   dw.K = padded ? up32(a.R) : a.R;
   dw.partial = reinterpret_cast<float*>(ws + p.off_pw);
   const int sx = a.grad_W ? p.dx : p.dx1, sw = a.grad_x ? p.dw : p.dw1;
-  if constexpr (std::is_same<TI, float>::value) launch_backward<Fp32, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
+  if constexpr (std::is_same<TI, float>::value) launch_backward<Fp32Back, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
   else if (p.wide) launch_backward<Bf16Wide, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
   else launch_backward<Bf16, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
 }

@@ -231,6 +231,30 @@ def test_residual_layer_in_place():
         assert torch.equal(a, gx)
 
 
+@pytest.mark.parametrize("R,I,O", [(40, 100, 50), (700, 700, 900), (300, 4500, 400)])
+def test_fp32_rows_of_any_scale(R, I, O):
+    """Rows of x and W that are fifteen orders of magnitude apart, and values eight orders apart inside each: every result is as
+    exact as its own terms allow.  An infinite value makes its row NaN and no other."""
+    import torch
+    rng = np.random.default_rng(R)
+    spread = lambda n, m: rng.normal(size=(n, m)) * 10.0 ** rng.uniform(-8, 0, size=(n, m)) * 10.0 ** rng.uniform(-15, 15, size=(n, 1))
+    x, W = rounded(spread(R, I), False), rounded(spread(O, I), False)
+    x[3] = 0.0
+    cfg = bd.make_dense_config(R, I, O)
+    f = torch.float32
+    y, ws = torch.empty(R, O, device="cuda:0"), workspace(cfg)
+    tx, tW = put(x, f), put(W, f)
+    bd.spcfg_dense_forward(cfg, tx, tW, None, None, y, None, ws)
+    want = x @ W.T
+    close("y", values(y), want, product_tol(x, W) + 2.0 ** -24 * np.abs(want) + 2.0 ** -126)
+    tx[5, 7] = float("inf")
+    bd.spcfg_dense_forward(cfg, tx, tW, None, None, y, None, ws)
+    got = values(y)
+    assert np.all(np.isnan(got[5]))
+    rest = np.arange(R) != 5
+    close("other rows", got[rest], want[rest], (product_tol(x, W) + 2.0 ** -24 * np.abs(want) + 2.0 ** -126)[rest])
+
+
 def test_activations_of_extreme_values():
     """Infinite and huge sums reach the activation as they are (bf16 operands); slopes there are 0 or 1; NaN stays NaN."""
     import torch
