@@ -13,7 +13,7 @@
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
 //    32 or 64 values of k: rows of 64 or 128 bytes along k, with the 16-byte piece XORed with bits 2..3, resp. 1..3 of the
-//    row; across k rows of 128 columns, with the 64-byte piece XORed with the row mod 4.  Operands come out of LDS with
+//    row; across k rows of 128 or 64 columns, with the 64-byte piece XORed with the row mod 4, resp. bit 1 of it.  Operands come out of LDS with
 //    ds_read_b128, resp. with the transposing ds_read_b64_tr_b16; both forms meet no bank conflict.
 //  * The order of a step is written out: products of 16 k while the next 16 are read; behind the first products of the last 16
 //    the barrier - each wavefront's loads of the next step have landed, nobody needs this step's tiles any more - then the
@@ -76,6 +76,7 @@ template <int PL_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct 
   static constexpr int NA = PL == 2 ? 2 : 1;          // sums: fp16 planes keep the small products apart
   static constexpr int kLds = NS * STAGE;
   static_assert(LA % NW == 0 && LB % NW == 0, "loads of a plane's tile are dealt evenly");
+  static_assert((BM < 128) == (BN < 128), "panels across k are as wide for both operands");
   static_assert((ME == 32 || ME == 64) && (PL != 2 || BK == 32) && NS >= 2 && ND * (NS - 1) < 64, "");
 };
 
@@ -130,14 +131,16 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   const int k0 = split * p.steps_per_split, k1 = min(p.steps, k0 + p.steps_per_split);
 
   // this wavefront's loads: entry e of [A planes | B planes], 1 KB each.  Along k: 16 rows of 64 or 8 of 128 bytes; across: 4
-  // of 256, ME rows of 128 columns after the other.
+  // of 256 (8 of 128 in tiles of 64), ME rows of one panel of 128 (64) columns after those of the other.
   // Addresses are a base per operand and plane, the same for all lanes, plus 32 bits (the host checks that these do).
   const unsigned lds0 = lds_address(lds);
   unsigned e_off[ND], e_lds[ND];
-  constexpr int RL = 1024 / S::RB, QA = ME / 4;  // rows of a load along k; loads of 128 columns across k
+  constexpr int RL = 1024 / S::RB;                               // rows of a load along k
+  constexpr int PW = S::BM < 128 ? 64 : 128, RP = 512 / PW, QA = ME / RP;  // across: columns of a panel, rows of a load, loads of a panel
   // row of those, and piece: XOR with bits of the row (the loads of a plane are RL rows apart, a multiple of 8)
   const int r_al = lane / (64 / RL), c_al = (lane & (64 / RL - 1)) ^ (ME == 32 ? (r_al >> 2) & 3 : 0);
-  const int r_ac = lane >> 4, c_ac = (((lane & 15) >> 2) ^ r_ac) * 32 + (lane & 3) * 8;
+  const int r_ac = lane / (64 / RP), key_ac = PW == 128 ? r_ac & 3 : (r_ac >> 1) & 1;
+  const int c_ac = ((lane % (64 / RP) >> 2) ^ key_ac) * 32 + (lane & 3) * 8;
   static_for<0, ND>([&](auto j) {
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
@@ -146,8 +149,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     e_lds[jv] = (unsigned)((isA ? plane * S::PTA : MP * S::PTA + plane * S::PTB) + q * 1024);
     const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
     if constexpr (isA ? TA : TB) {
-      const int64_t col = min(o0 + q / QA * 128 + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
-      e_off[jv] = (unsigned)(2 * ((4 * (q % QA) + r_ac) * ld + col));
+      const int64_t col = min(o0 + q / QA * PW + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
+      e_off[jv] = (unsigned)(2 * ((RP * (q % QA) + r_ac) * ld + col));
     } else {
       const int piece = ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7);
       e_off[jv] = (unsigned)(2 * (min(o0 + RL * q + r_al, len - 1) - o0) * ld + 16 * piece);
@@ -187,7 +190,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       constexpr bool isA = jv < S::NDA;
       constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
       const int q = wave + e0 % per;
-      const int k = (isA ? TA : TB) ? 4 * (q % QA) + r_ac : 8 * (ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
+      const int k = (isA ? TA : TB) ? RP * (q % QA) + r_ac : 8 * (ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
       const unsigned char* at = base[isA ? 0 : 1][plane] + e_off[jv];
       dma16(k < last_left ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
     });
@@ -199,12 +202,14 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     const int fr = lane & 31, fh = lane >> 5;
     const unsigned al = (unsigned)(fr * S::RB + (fh ^ (ME == 32 ? (fr >> 2) & 3 : (fr >> 1) & 7)) * 16);
     const int li = lane & 15, lq = lane >> 4;
-    const unsigned ac = (unsigned)((8 * (lq >> 1) + (li >> 2)) * 256 + 32 * (lq & 1) + 8 * (li & 3));
+    const unsigned ac = (unsigned)((8 * (lq >> 1) + (li >> 2)) * (2 * PW) + 32 * (lq & 1) + 8 * (li & 3));
+    const int key = PW == 128 ? li >> 2 : (li >> 3) & 1;
+    constexpr int PB = PW / 32;  // blocks of 32 columns of a panel
     if constexpr (TA) {
 #pragma unroll
       for (int f = 0; f < MI; ++f) {
         const int blk = wm * MI + f;
-        fa[f] = ac + (unsigned)((blk >> 2) * (ME * 256) + (((blk & 3) ^ (li >> 2)) * 64));
+        fa[f] = ac + (unsigned)(blk / PB * (ME * 2 * PW) + ((blk % PB) ^ key) * 64);
       }
     } else {
       fa[0] = al + (unsigned)(wm * MI * 32 * S::RB);
@@ -213,7 +218,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 #pragma unroll
       for (int f = 0; f < NI; ++f) {
         const int blk = wn * NI + f;
-        fb[f] = MP * S::PTA + ac + (unsigned)((blk >> 2) * (ME * 256) + (((blk & 3) ^ (li >> 2)) * 64));
+        fb[f] = MP * S::PTA + ac + (unsigned)(blk / PB * (ME * 2 * PW) + ((blk % PB) ^ key) * 64);
       }
     } else {
       fb[0] = MP * S::PTA + al + (unsigned)(wn * NI * 32 * S::RB);
@@ -231,8 +236,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       constexpr int pl = rv / MI, f = rv % MI;
       if constexpr (TA) {
         const unsigned at = lds0 + stage + fa[f];
-        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].lo) : "v"(at), "n"(pl * S::PTA + cv * 4096));
-        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 4096 + 1024));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].lo) : "v"(at), "n"(pl * S::PTA + cv * 32 * PW));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 32 * PW + 8 * PW));
       } else {
         const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
         asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTA) + f * 32 * S::RB));
@@ -241,8 +246,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       constexpr int pl = (rv - PL * MI) / NI, f = (rv - PL * MI) % NI;
       if constexpr (TB) {
         const unsigned at = lds0 + stage + fb[f];
-        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].lo) : "v"(at), "n"(pl * S::PTB + cv * 4096));
-        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 4096 + 1024));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].lo) : "v"(at), "n"(pl * S::PTB + cv * 32 * PW));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 32 * PW + 8 * PW));
       } else {
         const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
         asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTB) + f * 32 * S::RB));
@@ -330,6 +335,10 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     const bool more = i + NS < n && k0 + i + NS < whole;
     if (i + NS < n && k0 + i + NS >= whole) load_last(cur);
     SPCFG_SB
+    if constexpr (RS == 0) {  // (a single product a chunk: nothing to put them between)
+      static_for<0, NF>([&](auto r) { read_one(X, r, nxt, std::integral_constant<int, 0>{}); });
+      if (more) static_for<0, ND>([&](auto j) { load_one(j, cur); });
+    }
     static_for<NB, NM>([&](auto m) {
       constexpr int s = decltype(m)::value - NB;
       mfma_one(Y, m);
@@ -654,28 +663,32 @@ __global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
 // ---- which form, and what it needs -----------------------------------------------------------------------------------------
 int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
 
-// A product as tiles of t x t that go through all of k: `n` of them, of `steps` steps.
+// A product as tiles that go through all of k: `n` of them, of `steps` steps.
 struct Work { int64_t n, steps; };
-Work work_of(int64_t M, int64_t N, int64_t K, int t, int bk) { return Work{tiles(M, t) * tiles(N, t), tiles(K, bk)}; }
 
-// Into how many workgroups each tile's steps are cut, for two products of one launch (or one, b.n = 0).  What the launch takes
-// is estimated in us: `step` a step, the longest share where all of `room` workgroups run at once, the mean with half a share on
-// top where they do not; splitting costs a launch more (3 us) and partial tiles of `tile` values written and read again at
-// 4 TB/s.  Of the share lengths that cut the longer product into 1, 2, 3, ... the best is taken; a share has at least
-// `least` steps.  Measured: 4096 x 512 x 512 in fp32 (128 tiles of 16 steps) in two 37 us, in one 25.
-void choose_splits(Work a, Work b, int64_t room, int64_t least, double step, int64_t tile, int* sa, int* sb) {
-  double best = 1e30;
-  const int64_t longer = b.n && b.steps > a.steps ? b.steps : a.steps;
-  for (int64_t s = 1; s <= 32 && (s == 1 || longer / s >= least); ++s) {
-    const int64_t len = tiles(longer, (int)s), pa = tiles(a.steps, (int)len), pb = b.n ? tiles(b.steps, (int)len) : 0;
-    const int64_t la = tiles(a.steps, (int)pa), lb = pb ? tiles(b.steps, (int)pb) : 0, wgs = a.n * pa + b.n * pb;
-    const double most = (double)(la > lb ? la : lb), mean = (double)(a.n * pa * la + b.n * pb * lb) / room;
-    double t = wgs <= room ? most : mean + 0.5 * most;
-    if (t < most) t = most;
-    t *= step;
-    const int64_t parts = (pa > 1 ? a.n * pa : 0) + (pb > 1 ? b.n * pb : 0);
-    if (parts) t += 3 + 2e-6 * parts * tile;
-    if (t < best) { best = t; *sa = (int)pa; *sb = (int)(pb ? pb : 1); }
+// Tiles of t x t, `room` workgroups at a time on the chip, `step` us a step of bk where it is full, shares of `least` steps or more.
+struct Tiling { int t, bk, room, least; double step; };
+struct Choice { int t, sa, sb; double us; };
+
+// Into how many workgroups each tile's steps are cut, for two products of one launch (or one, the other of no size), with one
+// tiling.  A workgroup takes 3.5 us to start and end, and its steps; the launch is estimated as the longest where all run at
+// once, as the mean with half the longest on top where they do not; splitting costs a launch more (3 us) and partial tiles
+// written and read again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
+// Measured: 4096 x 512 x 512 in fp32 (128 tiles of 128 x 128, 16 steps) in two 37 us, in one 30.
+void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Choice* best) {
+  auto work = [&](const int64_t (&d)[3]) { return Work{d[2] ? tiles(d[0], g.t) * tiles(d[1], g.t) : 0, tiles(d[2], g.bk)}; };
+  const Work wa = work(a), wb = work(b);
+  const int64_t longer = wb.steps > wa.steps ? wb.steps : wa.steps;
+  for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    if (s > 1 && longer < (int64_t)s * g.least) break;
+    const int64_t len = tiles(longer, s), pa = wa.n ? tiles(wa.steps, (int)len) : 0, pb = wb.n ? tiles(wb.steps, (int)len) : 0;
+    const double ta = pa ? 3.5 + g.step * tiles(wa.steps, (int)pa) : 0, tb = pb ? 3.5 + g.step * tiles(wb.steps, (int)pb) : 0;
+    const double most = ta > tb ? ta : tb, mean = (wa.n * pa * ta + wb.n * pb * tb) / g.room;
+    double us = wa.n * pa + wb.n * pb <= g.room ? most : mean + 0.5 * most;
+    if (us < most) us = most;
+    const int64_t parts = (pa > 1 ? wa.n * pa : 0) + (pb > 1 ? wb.n * pb : 0);
+    if (parts) us += 3 + 2e-6 * parts * g.t * g.t;
+    if (us < best->us) *best = Choice{g.t, (int)(pa ? pa : 1), (int)(pb ? pb : 1), us};
   }
 }
 
@@ -684,27 +697,27 @@ bool large(int64_t R, int64_t I, int64_t O) {
   return R * I * O >= ((int64_t)1 << 28) && R >= 64 && I >= 64 && O >= 64 && R < most && I < most && O < most;
 }
 
+// What a call does and where it keeps it.
 struct Plan {
   bool on;                 // whether the layer takes tiled products at all
-  bool wide;               // tiles of 256 x 256 (all products of the call)
   bool cut;                // x and W as planes (fp32, or rows that do not lie on 16 bytes)
   bool dz;                 // dz as planes
-  int pl;
   int64_t x, w, z;         // elements of one plane of x, W, dz
   int span, parts;         // rows of a part of the bias's gradient
-  int fwd, dx, dw;         // splits; dx1, dw1 where the other product of the backward pass is not wanted
-  int dx1, dw1;
-  size_t off_x, off_w, off_e, off_z, off_sums, off_px, off_pw, bytes;
+  Choice c;
+  size_t off_x, off_w, off_e, off_z, off_sums, off_pa, off_pb, bytes;
 };
 
-Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
+enum { FORWARD = 0, BACK_X = 1, BACK_W = 2, BACK = 3 };
+
+Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act, int what) {
   Plan p{};
   p.on = R > 0 && large(R, I, O);
   if (!p.on) return p;
   const bool fp32 = in_type == SPCFG_TYPE_F32;
-  p.pl = fp32 ? 3 : 1;
+  const int pl = fp32 ? 3 : 1;
   p.cut = fp32 || I % 8 != 0;
-  p.dz = fp32 || out_type == SPCFG_TYPE_F32 || act != SPCFG_ACT_NONE || O % 8 != 0;
+  p.dz = what != FORWARD && (fp32 || out_type == SPCFG_TYPE_F32 || act != SPCFG_ACT_NONE || O % 8 != 0);
   p.x = up32(R) * up32(I);
   p.w = up32(O) * up32(I);
   p.z = up32(R) * up32(O);
@@ -713,36 +726,31 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   if (span < 16) span = 16;
   p.span = (int)span;
   p.parts = (int)tiles(up32(R), p.span);
-  // wide tiles: a CU's worth of them for every CU and sums long enough to make up for their longer start and end
-  // (8192 x 4096 x 4096: 241 us, 320 on 128 x 128; 2048 x 512 x 10000: 61 us, 43)
-  p.wide = !fp32 && tiles(R, 256) * tiles(O, 256) >= 256 && I >= 2048;
-  const int t = p.wide ? 256 : 128, bk = fp32 ? 32 : 64;
-  const int64_t room_f = p.wide ? 256 : 512, room = fp32 || p.wide ? 256 : 512, least = fp32 ? 6 : 3;
-  // us a step where every CU has as many workgroups as it holds
-  const double step_f = p.wide ? 0.95 : 0.6, step = fp32 ? 1.2 : step_f;
-  int none;
-  const Work wf = work_of(R, O, I, t, bk), wx = work_of(R, I, O, t, bk), ww = work_of(O, I, R, t, bk), w0{0, 0};
-  choose_splits(wf, w0, room_f, least, step_f, t * t, &p.fwd, &none);
-  choose_splits(wx, ww, room, least, step, t * t, &p.dx, &p.dw);
-  choose_splits(wx, w0, room, least, step, t * t, &p.dx1, &none);
-  choose_splits(ww, w0, room, least, step, t * t, &p.dw1, &none);
+  const int64_t none[3] = {0, 0, 0}, f[3] = {R, O, I}, x[3] = {R, I, O}, w[3] = {O, I, R};
+  const int64_t(&da)[3] = what == FORWARD ? f : what & BACK_X ? x : none;
+  const int64_t(&db)[3] = what & BACK_W ? w : none;
+  p.c.us = 1e30;
+  if (fp32 && what == FORWARD) {
+    consider(Tiling{64, 32, 512, 8, 0.32}, da, db, &p.c);
+    consider(Tiling{128, 32, 512, 6, 0.7}, da, db, &p.c);
+  } else if (fp32) {
+    consider(Tiling{64, 32, 512, 8, 0.5}, da, db, &p.c);
+    consider(Tiling{128, 32, 256, 6, 1.1}, da, db, &p.c);
+  } else {
+    consider(Tiling{64, 64, 512, 4, 0.3}, da, db, &p.c);
+    consider(Tiling{128, 64, 512, 3, 0.6}, da, db, &p.c);
+    consider(Tiling{256, 64, 256, 3, 0.85}, da, db, &p.c);
+  }
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
-  auto partial = [&](int splits, int more, int64_t M, int64_t N) {
-    const int s = splits > more ? splits : more;
-    return s > 1 ? (size_t)s * M * N * 4 : 0;
-  };
-  p.off_x = take(p.cut ? (size_t)p.x * 2 * p.pl : 0);
-  p.off_w = take(p.cut ? (size_t)p.w * 2 * p.pl : 0);
-  p.off_e = take(fp32 ? (size_t)(R + O) * 4 : 0);
-  const size_t forward_part = at;
-  p.off_z = take(p.dz ? (size_t)p.z * 2 * p.pl : 0);
-  p.off_sums = take((size_t)p.parts * O * 4);
-  p.off_px = take(partial(p.dx, p.dx1, R, I));
-  p.off_pw = take(partial(p.dw, p.dw1, O, I));
-  // the forward product's partial tiles lie where the backward pass keeps dz and its own
-  const size_t fwd_end = forward_part + partial(p.fwd, 1, R, O);
-  p.bytes = at > fwd_end ? at : (fwd_end + 255) / 256 * 256;
+  p.off_x = take(p.cut ? (size_t)p.x * 2 * pl : 0);
+  p.off_w = take(p.cut ? (size_t)p.w * 2 * pl : 0);
+  p.off_e = take(fp32 && what == FORWARD ? (size_t)(R + O) * 4 : 0);
+  p.off_z = take(p.dz ? (size_t)p.z * 2 * pl : 0);
+  p.off_sums = take(what != FORWARD ? (size_t)p.parts * O * 4 : 0);
+  p.off_pa = take(p.c.sa > 1 ? (size_t)p.c.sa * da[0] * da[1] * 4 : 0);
+  p.off_pb = take(p.c.sb > 1 ? (size_t)p.c.sb * db[0] * db[1] * 4 : 0);
+  p.bytes = at;
   return p;
 }
 
@@ -776,18 +784,28 @@ void launch_backward(const Args& a, Product x, Product w, int sx, int sw, const 
   if (jx + jw) hipLaunchKernelGGL((k_dense_backward_join<TI, TO>), dim3(jx + jw), dim3(256), 0, st, a, x, w, jx);
 }
 
-// The shapes: two wavefronts per SIMD, one issuing while the other waits
-using Fp32 = Shape<2, 128, 128, 2, 4, 32, 2>;      // forward
-using Fp32Back = Shape<3, 128, 128, 2, 4, 32, 3>;
-using Bf16 = Shape<1, 128, 128, 2, 4, 64, 2>;
-using Bf16Wide = Shape<1, 256, 256, 2, 4, 64, 2>;
+// The shapes of a type's products: tiles of 64, 128 and (bf16) 256; at 128 and 256 two wavefronts per SIMD and workgroup, one
+// issuing while the other waits
+template <typename TI, bool BACKWARD> struct Shapes {
+  using T64 = Shape<1, 64, 64, 2, 2, 64, 4>;
+  using T128 = Shape<1, 128, 128, 2, 4, 64, 2>;
+  using T256 = Shape<1, 256, 256, 2, 4, 64, 2>;
+};
+template <> struct Shapes<float, false> {
+  using T64 = Shape<2, 64, 64, 2, 2, 32, 4>;
+  using T128 = Shape<2, 128, 128, 2, 4, 32, 2>;
+};
+template <> struct Shapes<float, true> {
+  using T64 = Shape<3, 64, 64, 2, 2, 32, 3>;
+  using T128 = Shape<3, 128, 128, 2, 4, 32, 3>;
+};
 
 template <typename TI, typename TO>
 void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   Product q{};
   q.M = a.R;
   q.N = a.O;
-  q.partial = reinterpret_cast<float*>(ws + p.off_z);
+  q.partial = reinterpret_cast<float*>(ws + p.off_pa);
   if constexpr (std::is_same<TI, float>::value) {
     Halves h{};
     h.src[0] = static_cast<const float*>(a.x); h.src[1] = static_cast<const float*>(a.W);
@@ -814,9 +832,12 @@ void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
     q.A = static_cast<const uint16_t*>(a.x); q.B = static_cast<const uint16_t*>(a.W);
     q.lda = q.ldb = q.K = a.I;
   }
-  if constexpr (std::is_same<TI, float>::value) launch_forward<Fp32, TI, TO>(a, q, p.fwd, st);
-  else if (p.wide) launch_forward<Bf16Wide, TI, TO>(a, q, p.fwd, st);
-  else launch_forward<Bf16, TI, TO>(a, q, p.fwd, st);
+  using S = Shapes<TI, false>;
+  if (p.c.t == 64) return launch_forward<typename S::T64, TI, TO>(a, q, p.c.sa, st);
+  if constexpr (!std::is_same<TI, float>::value) {
+    if (p.c.t == 256) return launch_forward<typename S::T256, TI, TO>(a, q, p.c.sa, st);
+  }
+  launch_forward<typename S::T128, TI, TO>(a, q, p.c.sa, st);
 }
 
 template <typename TI, typename TO>
@@ -848,26 +869,33 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   dx.B = W; dx.ldb = ldi; dx.plane_b = p.w;
   dx.M = a.R; dx.N = a.I;
   dx.K = padded ? up32(a.O) : a.O;
-  dx.partial = reinterpret_cast<float*>(ws + p.off_px);
+  dx.partial = reinterpret_cast<float*>(ws + p.off_pa);
   dw.A = z; dw.lda = ldo; dw.plane_a = p.z;
   dw.B = x; dw.ldb = ldi; dw.plane_b = p.x;
   dw.M = a.O; dw.N = a.I;
   dw.K = padded ? up32(a.R) : a.R;
-  dw.partial = reinterpret_cast<float*>(ws + p.off_pw);
-  const int sx = a.grad_W ? p.dx : p.dx1, sw = a.grad_x ? p.dw : p.dw1;
-  if constexpr (std::is_same<TI, float>::value) launch_backward<Fp32Back, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
-  else if (p.wide) launch_backward<Bf16Wide, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
-  else launch_backward<Bf16, TI, TO>(a, dx, dw, sx, sw, r.sums, p.parts, st);
+  dw.partial = reinterpret_cast<float*>(ws + p.off_pb);
+  using S = Shapes<TI, true>;
+  if (p.c.t == 64) return launch_backward<typename S::T64, TI, TO>(a, dx, dw, p.c.sa, p.c.sb, r.sums, p.parts, st);
+  if constexpr (!std::is_same<TI, float>::value) {
+    if (p.c.t == 256) return launch_backward<typename S::T256, TI, TO>(a, dx, dw, p.c.sa, p.c.sb, r.sums, p.parts, st);
+  }
+  launch_backward<typename S::T128, TI, TO>(a, dx, dw, p.c.sa, p.c.sb, r.sums, p.parts, st);
 }
 
 }  // namespace
 
 size_t tiled_workspace(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act) {
-  return plan_of(R, I, O, in_type, out_type, act).bytes;
+  size_t most = 0;
+  for (int what : {FORWARD, BACK_X, BACK_W, BACK}) {
+    const size_t n = plan_of(R, I, O, in_type, out_type, act, what).bytes;
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st) {
-  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act);
+  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act, FORWARD);
   if (!p.on || (!p.cut && (!on16(a.x) || !on16(a.W)))) return false;
   char* w = static_cast<char*>(ws);
   if (in_type == SPCFG_TYPE_F32) forward<float, float>(a, p, w, st);
@@ -877,7 +905,7 @@ bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream
 }
 
 bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st) {
-  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act);
+  const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act, (a.grad_x ? BACK_X : 0) | (a.grad_W ? BACK_W : 0));
   if (!p.on || (!p.cut && (!on16(a.x) || !on16(a.W))) || (!p.dz && !on16(a.grad_y))) return false;
   char* w = static_cast<char*>(ws);
   if (in_type == SPCFG_TYPE_F32) backward<float, float>(a, p, w, st);
