@@ -221,12 +221,18 @@ __device__ __forceinline__ void store_bias(const Args& g, int64_t m, float s) {
 
 inline bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// what a call computes: FORWARD, or of the backward pass dx, dW or both
+enum { FORWARD = 0, BACK_X = 1, BACK_W = 2, BACK = 3 };
+
+// Products in registers (dense_direct.hip), for any sizes, types and alignments; an estimate of what they take
+double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int what);
 void launch_direct_forward(const Args& a, int in_type, int out_type, hipStream_t st);
 void launch_direct_backward(const Args& a, int in_type, int out_type, hipStream_t st);
 
-// Tiled products (dense_tile.hip): workspace of a layer, 0 where none of its products takes them
+// Tiled products (dense_tile.hip): workspace of a layer, 0 where it never takes them
 size_t tiled_workspace(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act);
-// whether these take the call: sizes, and alignment of what is read as it lies
+// whether these take the call: where they are estimated to be faster than products in registers, and what is read as it lies is on
+// 16 bytes
 bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
 bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
 

@@ -666,15 +666,17 @@ int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
 // A product as tiles that go through all of k: `n` of them, of `steps` steps.
 struct Work { int64_t n, steps; };
 
-// Tiles of t x t, `room` workgroups at a time on the chip, `step` us a step of bk where it is full, shares of `least` steps or more.
-struct Tiling { int t, bk, room, least; double step; };
+// Tiles of t x t: `room` workgroups at a time on the chip, `start` us to start and end one, `wait` us a step of bk that it takes
+// alone (latency), `busy` us a step of one per CU at full rate, shares of `least` steps or more.
+struct Tiling { int t, bk, room, least; double start, wait, busy; };
 struct Choice { int t, sa, sb; double us; };
 
 // Into how many workgroups each tile's steps are cut, for two products of one launch (or one, the other of no size), with one
-// tiling.  A workgroup takes 3.5 us to start and end, and its steps; the launch is estimated as the longest where all run at
-// once, as the mean with half the longest on top where they do not; splitting costs a launch more (3 us) and partial tiles
-// written and read again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
-// Measured: 4096 x 512 x 512 in fp32 (128 tiles of 128 x 128, 16 steps) in two 37 us, in one 30.
+// tiling.  A step takes what it takes alone or its share of the CU, whichever is longer; the launch is estimated as the longest
+// workgroup where all run at once, as their mean with half the longest on top where they do not; splitting costs a launch more (6 us) and partial tiles written and read
+// again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
+// Measured (us): 4096 x 512 x 512 in fp32 (128 tiles of 128 x 128, 16 steps) in two 37, in one 30, on 64 x 64 24;
+// bf16 8192 x 4096 x 4096 on 256 x 256 241, on 128 x 128 320; 2048 x 512 x 10000 61, 43; 512^3 on 128 x 128 9.7, on 64 x 64 6.9.
 void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Choice* best) {
   auto work = [&](const int64_t (&d)[3]) { return Work{d[2] ? tiles(d[0], g.t) * tiles(d[1], g.t) : 0, tiles(d[2], g.bk)}; };
   const Work wa = work(a), wb = work(b);
@@ -682,19 +684,16 @@ void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Cho
   for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
     if (s > 1 && longer < (int64_t)s * g.least) break;
     const int64_t len = tiles(longer, s), pa = wa.n ? tiles(wa.steps, (int)len) : 0, pb = wb.n ? tiles(wb.steps, (int)len) : 0;
-    const double ta = pa ? 3.5 + g.step * tiles(wa.steps, (int)pa) : 0, tb = pb ? 3.5 + g.step * tiles(wb.steps, (int)pb) : 0;
+    const double wgs = (double)(wa.n * pa + wb.n * pb), here = (wgs < g.room ? wgs : g.room) / 256;
+    const double step = here * g.busy > g.wait ? here * g.busy : g.wait;
+    const double ta = pa ? g.start + step * tiles(wa.steps, (int)pa) : 0, tb = pb ? g.start + step * tiles(wb.steps, (int)pb) : 0;
     const double most = ta > tb ? ta : tb, mean = (wa.n * pa * ta + wb.n * pb * tb) / g.room;
-    double us = wa.n * pa + wb.n * pb <= g.room ? most : mean + 0.5 * most;
+    double us = wgs <= g.room ? most : mean + 0.5 * most;
     if (us < most) us = most;
     const int64_t parts = (pa > 1 ? wa.n * pa : 0) + (pb > 1 ? wb.n * pb : 0);
-    if (parts) us += 3 + 2e-6 * parts * g.t * g.t;
+    if (parts) us += 6 + 2e-6 * parts * g.t * g.t;
     if (us < best->us) *best = Choice{g.t, (int)(pa ? pa : 1), (int)(pb ? pb : 1), us};
   }
-}
-
-bool large(int64_t R, int64_t I, int64_t O) {
-  const int64_t most = 1 << 22;  // offsets inside a tile (256 rows, or 32 rows across k) fit 32 bits
-  return R * I * O >= ((int64_t)1 << 28) && R >= 64 && I >= 64 && O >= 64 && R < most && I < most && O < most;
 }
 
 // What a call does and where it keeps it.
@@ -708,12 +707,10 @@ struct Plan {
   size_t off_x, off_w, off_e, off_z, off_sums, off_pa, off_pb, bytes;
 };
 
-enum { FORWARD = 0, BACK_X = 1, BACK_W = 2, BACK = 3 };
-
 Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act, int what) {
   Plan p{};
-  p.on = R > 0 && large(R, I, O);
-  if (!p.on) return p;
+  const int64_t most = 1 << 22;  // offsets inside a tile (256 rows, or 64 rows across k) fit 32 bits
+  if (R < 1 || R >= most || I >= most || O >= most) return p;
   const bool fp32 = in_type == SPCFG_TYPE_F32;
   const int pl = fp32 ? 3 : 1;
   p.cut = fp32 || I % 8 != 0;
@@ -731,16 +728,24 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   const int64_t(&db)[3] = what & BACK_W ? w : none;
   p.c.us = 1e30;
   if (fp32 && what == FORWARD) {
-    consider(Tiling{64, 32, 512, 8, 0.32}, da, db, &p.c);
-    consider(Tiling{128, 32, 512, 6, 0.7}, da, db, &p.c);
+    consider(Tiling{64, 32, 512, 8, 5, 0.31, 0.29}, da, db, &p.c);
+    consider(Tiling{128, 32, 512, 6, 5, 0.95, 0.8}, da, db, &p.c);
   } else if (fp32) {
-    consider(Tiling{64, 32, 512, 8, 0.5}, da, db, &p.c);
-    consider(Tiling{128, 32, 256, 6, 1.1}, da, db, &p.c);
+    consider(Tiling{64, 32, 512, 8, 5, 0.45, 0.39}, da, db, &p.c);
+    consider(Tiling{128, 32, 256, 6, 5, 1.2, 1.25}, da, db, &p.c);
   } else {
-    consider(Tiling{64, 64, 512, 4, 0.3}, da, db, &p.c);
-    consider(Tiling{128, 64, 512, 3, 0.6}, da, db, &p.c);
-    consider(Tiling{256, 64, 256, 3, 0.85}, da, db, &p.c);
+    consider(Tiling{64, 64, 512, 4, 5, 0.3, what == FORWARD ? 0.3 : 0.25}, da, db, &p.c);
+    consider(Tiling{128, 64, 512, 3, 5, 0.75, 0.67}, da, db, &p.c);
+    consider(Tiling{256, 64, 256, 3, 15, 1.5, 1.75}, da, db, &p.c);
   }
+  // beside the products: a launch for planes and dz, 3 us and its bytes at 4 TB/s
+  const double si = fp32 ? 4 : 2, so = out_type == SPCFG_TYPE_F32 ? 4 : 2;
+  double bytes = 0;
+  if (p.cut) bytes += (what != BACK_X ? (double)R * I : 0) * (fp32 && what == FORWARD ? 8 : si * 2.5) + (what != BACK_W ? (double)O * I : 0) * (fp32 && what == FORWARD ? 8 : si * 2.5);
+  if (what != FORWARD) bytes += (double)R * O * ((act ? 2 : 1) * so + (p.dz ? 2 * pl : 0));
+  const double us = p.c.us + (bytes > 0 ? 3 + bytes / 4e6 : 0);
+  p.on = us < direct_us(R, I, O, in_type, what);
+  if (!p.on) return p;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
   p.off_x = take(p.cut ? (size_t)p.x * 2 * pl : 0);
