@@ -496,21 +496,23 @@ __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t, const float (
   *reinterpret_cast<uintx4*>(dst) = h;
 }
 
-// eight values of a row from column c on, zero outside the matrix
+// eight values of a row from column c on, zero outside the matrix (where the nearest ones inside are loaded: no load hangs on a
+// branch of its own)
 template <typename T>
 __device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, bool vec, float (&v)[8]) {
   T x[8];
-  if (vec && r < rows && c + 8 <= cols) {
+  const T* row = src + min(r, rows - 1) * cols;
+  if (vec) {  // (cols is a multiple of 8)
     uintx4 w[sizeof(T) / 2];
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uintx4*>(src + r * cols + c)[i];
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uintx4*>(row + min(c, cols - 8))[i];
     __builtin_memcpy(x, w, sizeof(x));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = r < rows && c + i < cols ? src[r * cols + c + i] : T(0);
+    for (int i = 0; i < 8; ++i) x[i] = row[min(c + i, cols - 1)];
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = to_float<T>(x[i]);
+  for (int i = 0; i < 8; ++i) v[i] = r < rows && c + i < cols ? to_float<T>(x[i]) : 0.0f;
 }
 
 // Planes of one matrix, eight values a thread.
@@ -526,7 +528,7 @@ __device__ __forceinline__ void cut(const T* __restrict__ src, uint16_t* __restr
     r = e / ld;
     c = e - r * ld;
   }
-  const bool vec = ((((uintptr_t)src) | (uintptr_t)(cols * sizeof(T))) & 15) == 0;
+  const bool vec = ((uintptr_t)src & 15) == 0 && (cols & 7) == 0;
   float v[8];
   eight<T>(src, rows, cols, r, c, vec, v);
   put_planes(dst + e, rows32 * ld, v, T());
@@ -544,7 +546,7 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
   const int64_t r1 = min(rows32, (int64_t)(part + 1) * span);
   const TO* gy = static_cast<const TO*>(g.grad_y);
   const TO* z = static_cast<const TO*>(g.preact_in);
-  const bool vec = ((((uintptr_t)gy) | ((uintptr_t)z) | (uintptr_t)(g.O * sizeof(TO))) & 15) == 0;
+  const bool vec = (((uintptr_t)gy | (uintptr_t)z) & 15) == 0 && (g.O & 7) == 0;
   float s[8] = {};
   if (c < ld) {
     // (four rows' loads in flight)
@@ -614,7 +616,7 @@ __global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
   if (r >= h.rows[w]) return;  // (whole groups at a time)
   const float* src = h.src[w];
   const int64_t cols = h.cols, ld = (cols + 31) / 32 * 32;
-  const bool vec = ((((uintptr_t)src) | (uintptr_t)(cols * 4)) & 15) == 0;
+  const bool vec = ((uintptr_t)src & 15) == 0 && (cols & 7) == 0;
   constexpr int E = 4;
   float v[E][8];
   float m = 0.0f;
