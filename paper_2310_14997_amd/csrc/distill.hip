@@ -4,7 +4,7 @@
 //   loss = tau^2 sum_e p_e (log p_e - log q_id(e)),         d loss / d s_j = tau (q_j - sum_{e: id(e) = j} p_e)
 // Bound by HBM: the row is read once and its gradient written once.  A row that a workgroup can hold in registers is one
 // pass; longer rows, and few rows, are split over workgroups along V: one launch leaves each part's maximum and sum of
-// exponentials, a second one joins them and writes the gradient.  Maxima, sums and p are in 32 bits; logarithms and the
+// exponentials (and, once a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p are in 32 bits; logarithms and the
 // sum over the teacher's entries, whose terms cancel where q is near p, in 64.
 #include <cmath>
 
@@ -37,29 +37,41 @@ struct Args {
   float *loss, *lse;
   const float* lse_in;
   void* grad;
-  float2* stat;         // [R][parts]: maximum, sum of exp((s - maximum) / tau)
+  struct RowTeacher* rec;  // [R] what the first launch of a split call leaves for the second
+  float2* stat;            // [R][parts]: maximum, sum of exp((s - maximum) / tau)
+};
+struct RowTeacher {
+  float top, inv;       // p = exp((t - top) / tau) * inv
+  int some, bad;
+  double terms, sum;    // sum of p (log p - s / tau), sum of p
 };
 
-// ---- sums and maxima over a workgroup of NT threads, in a fixed order ------------------------------------------------
-template <int NT, typename F, typename X>
-__device__ __forceinline__ X all(X v, X* red, F f) {
+// ---- sums and maxima over a workgroup of NT threads, N values at a time, in a fixed order --------------------------------
+template <typename F, typename X> __device__ __forceinline__ X across_wave(X v, F f) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
-  if (NT == 64) return v;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < NT / 64; ++i) v = f(v, red[i]);
   return v;
 }
-template <int NT, typename X> __device__ __forceinline__ X all_sum(X v, X* red) {
-  return all<NT>(v, red, [](X a, X b) { return a + b; });
+template <int NT, int N, typename F>
+__device__ __forceinline__ void all(float (&v)[N], float* red, F f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = across_wave(v[i], f);
+  if (NT == 64) return;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[i * 16 + (threadIdx.x >> 6)] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = red[i * 16];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) v[i] = f(v[i], red[i * 16 + w]);
+  }
 }
-template <int NT> __device__ __forceinline__ float all_max(float v, float* red) {
-  return all<NT>(v, red, [](float a, float b) { return fmaxf(a, b); });
-}
+struct Add { template <typename X> __device__ __forceinline__ X operator()(X a, X b) const { return a + b; } };
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 // ---- a row in vectors of 16 bytes -------------------------------------------------------------------------------------
 // Vector i holds the elements i * W - off .. + W - 1 of the row, off the row's offset from 16 bytes: whatever V and the
@@ -110,78 +122,101 @@ template <typename T> struct Row {
 // ---- the teacher's entries ---------------------------------------------------------------------------------------------
 struct Entries {
   alignas(16) int id[kMostEntries];  // -1 where absent, and up to the next multiple of 4
-  float p[kMostEntries];
+  float w[kMostEntries];             // the score, then exp((score - top) / tau)
 };
 struct Teacher {
-  bool some, bad;           // whether any entry is there; whether an id is out of range or a score NaN
-  double top, log_total;    // log p = t / tau - top - log_total
+  float top, inv;       // p = w * inv
+  bool some, bad;       // whether any entry is there; whether an id is out of range or a score NaN or +inf
 };
 
-// Fills E with the row's ids and p; an entry with a negative id or a score of -inf is absent.
+// Fills E with the row's ids and scores; an entry with a negative id or a score of -inf is absent.  This thread's share of the
+// largest score, and of whether something is wrong.
 template <typename T, int NT>
-__device__ Teacher teacher_row(const Args& g, int64_t row, Entries& E, float* red) {
+__device__ __forceinline__ void load_entries(const Args& g, int64_t row, Entries& E, float* top, float* wrong) {
   const T* t = static_cast<const T*>(g.teacher) + row * g.k;
   const int32_t* ids = g.ids + row * g.k;
-  float top = -INFINITY, wrong = 0.0f;
+  *top = -INFINITY;
+  *wrong = 0.0f;
   for (int e = threadIdx.x; e < g.k; e += NT) {
     int id = ids[e];
     const float a = to_float<T>(t[e]);
-    if (id >= 0 && (id >= g.V || a != a)) wrong = 1.0f;
+    if (id >= 0 && (id >= g.V || !(a < INFINITY))) *wrong = 1.0f;
     if (id >= g.V || a == -INFINITY) id = -1;
     E.id[e] = id < 0 ? -1 : id;
-    E.p[e] = a;
-    if (id >= 0) top = fmaxf(top, a);
+    E.w[e] = a;
+    if (id >= 0) *top = fmaxf(*top, a);
   }
   if (threadIdx.x < 3 && g.k + threadIdx.x < (unsigned)((g.k + 3) / 4 * 4)) E.id[g.k + threadIdx.x] = -1;
-  top = all_max<NT>(top, red);
-  wrong = all_max<NT>(wrong, red);
+}
+// E.w from scores to exponentials (each thread its own), and their sum over this thread's
+template <int NT>
+__device__ __forceinline__ float weigh_entries(const Args& g, Entries& E, float top) {
   float total = 0.0f;
   for (int e = threadIdx.x; e < g.k; e += NT) {
-    const float w = E.id[e] >= 0 ? expf((E.p[e] - top) * g.inv_tau) : 0.0f;
-    E.p[e] = w;
+    const float w = E.id[e] >= 0 ? expf((E.w[e] - top) * g.inv_tau) : 0.0f;
+    E.w[e] = w;
     total += w;
   }
-  total = all_sum<NT>(total, red);
-  Teacher r;
-  r.bad = wrong != 0.0f || !(total < INFINITY);
-  r.some = total > 0.0f || r.bad;
-  const float inv = 1.0f / total;
-  for (int e = threadIdx.x; e < g.k; e += NT) E.p[e] *= inv;
-  __syncthreads();
-  r.top = (double)top / g.tau;
-  r.log_total = log((double)total);
-  return r;
+  return total;
+}
+__device__ __forceinline__ Teacher teacher_of(float top, float wrong, float total) {
+  Teacher t;
+  t.top = top;
+  t.bad = wrong != 0.0f;
+  t.some = total > 0.0f || t.bad;
+  t.inv = 1.0f / total;
+  return t;
+}
+template <typename T, int NT>
+__device__ __forceinline__ Teacher teacher_row(const Args& g, int64_t row, Entries& E, float* red) {
+  float v[2];
+  load_entries<T, NT>(g, row, E, &v[0], &v[1]);
+  all<NT, 2>(v, red, Max());
+  float total[1] = {weigh_entries<NT>(g, E, v[0])};
+  all<NT, 1>(total, red, Add());
+  return teacher_of(v[0], v[1], total[0]);
 }
 
-// loss of the row on every thread: entries' terms summed in 64 bits
-template <typename T, int NT>
-__device__ float row_loss(const Args& g, int64_t row, const Entries& E, const Teacher& tr, double lse, double* red) {
+// One wavefront: sum of p (log p - s / tau) and of p over the row's entries, in 64 bits.  E is complete (behind a barrier).
+template <typename T>
+__device__ __forceinline__ void loss_terms(const Args& g, int64_t row, const Entries& E, const Teacher& tr, double* terms, double* sum) {
   const T* t = static_cast<const T*>(g.teacher) + row * g.k;
   const T* s = static_cast<const T*>(g.logits) + row * g.V;
-  double sum = 0.0;
-  for (int e = threadIdx.x; e < g.k; e += NT) {
+  const double inv_tau = 1.0 / g.tau, top = tr.top * inv_tau, log_inv = log((double)tr.inv);
+  double a = 0.0, b = 0.0;
+  for (int e = threadIdx.x & 63; e < g.k; e += 64) {
     const int id = E.id[e];
-    const double p = E.p[e];
-    if (id >= 0 && p > 0.0) {
-      const double log_p = (double)to_float<T>(t[e]) / g.tau - tr.top - tr.log_total;
-      sum += p * (log_p - ((double)to_float<T>(s[id]) / g.tau - lse));
+    const double p = id >= 0 ? (double)(E.w[e] * tr.inv) : 0.0;
+    if (p > 0.0) {
+      a += p * (to_float<T>(t[e]) * inv_tau - top + log_inv - to_float<T>(s[id]) * inv_tau);
+      b += p;
     }
   }
-  sum = all_sum<NT>(sum, red);
-  if (tr.bad) return NAN;
-  return tr.some ? (float)((double)g.tau * g.tau * sum) : 0.0f;
+  *terms = across_wave(a, Add());
+  *sum = across_wave(b, Add());
+}
+__device__ __forceinline__ float loss_of(const Args& g, bool some, bool bad, double terms, double sum, double lse) {
+  return bad ? NAN : some ? (float)((double)g.tau * g.tau * (terms + sum * lse)) : 0.0f;
 }
 
 // Gradient entries that the teacher has, for ids in [lo, hi): the first of equal ids writes what all of them add up to, in
-// their order.  The caller's other entries have been written before a barrier.
-template <typename T, int NT, typename Q>
-__device__ void write_entries(const Args& g, int64_t row, const Entries& E, float scale, int64_t lo, int64_t hi, Q q_of) {
-  T* o = static_cast<T*>(g.grad) + row * g.V;
-  for (int e = threadIdx.x; e < g.k; e += NT) {
-    const int id = E.id[e];
-    const bool mine = id >= 0 && id >= lo && id < hi;
-    if (!__any(mine)) continue;
-    const float q = mine ? q_of(id) : 0.0f;
+// their order.  What each thread's first entry takes - its score, and a look at all ids for equal ones - is done ahead
+// (look), while the rest of the row is under way; write comes when the other entries have been written, behind a barrier.
+template <typename T, int NT, typename P> struct Writer {
+  const Args& g;
+  const Entries& E;
+  const T* s;
+  int64_t lo, hi;
+  P p_of;               // p of entry e
+  float score, p;
+  bool first;
+  __device__ __forceinline__ Writer(const Args& g_, const Entries& E_, const T* s_, int64_t lo_, int64_t hi_, P p_of_)
+      : g(g_), E(E_), s(s_), lo(lo_), hi(hi_), p_of(p_of_) {}
+  __device__ __forceinline__ void look(int e) {
+    const int id = e < g.k ? E.id[e] : -1;
+    first = id >= 0 && id >= lo && id < hi;
+    if (!__any(first)) return;
+    if (first) score = to_float<T>(s[id]);
     // equal ids: any before this one, any behind it (four at a time; from k on there is no id)
     bool before = false, behind = false;
 #pragma unroll 4
@@ -194,50 +229,55 @@ __device__ void write_entries(const Args& g, int64_t row, const Entries& E, floa
         behind |= v[u] == id && f + u > e;
       }
     }
-    if (!mine || before) continue;
-    float p = E.p[e];
+    first = first && !before;
+    if (!first) return;
+    p = p_of(e);
     if (behind) {
       for (int f = e + 1; f < g.k; ++f)
-        if (E.id[f] == id) p += E.p[f];
+        if (E.id[f] == id) p += p_of(f);
     }
-    o[id] = from_float<T>(scale * (q - p));
   }
-}
+  // q_of(score): the softmax's entry
+  template <typename Q> __device__ __forceinline__ void write(T* o, float scale, Q q_of) {
+    for (int e = threadIdx.x; e < g.k; e += NT) {
+      if (e >= NT) look(e);
+      if (first) o[E.id[e]] = from_float<T>(scale * (q_of(score) - p));
+    }
+  }
+};
 
 // what the gradient of a row is scaled by; 0: the row is all zeros
-__device__ __forceinline__ float row_scale(const Args& g, int64_t row, const Teacher& tr) {
+__device__ __forceinline__ float row_scale(const Args& g, int64_t row, bool some, bool bad) {
   const float w = g.grad_loss ? g.grad_loss[row] : 1.0f;
-  if (w == 0.0f || !tr.some) return 0.0f;
-  return tr.bad ? NAN : w * g.tau;
+  if (w == 0.0f || !some) return 0.0f;
+  return bad ? NAN : w * g.tau;
 }
 
 // ---- a row per workgroup, in registers ----------------------------------------------------------------------------------
 template <typename T, int NT, int E, bool GRAD>
 __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   constexpr int W = Row<T>::W;
-  __shared__ float red[16];
-  __shared__ double redd[16];
+  __shared__ float red[48];
   __shared__ Entries ent;
   const int64_t row = blockIdx.x;
   const Row<T> s(g.logits, row, g.V);
   const int64_t nv = s.vectors();
   float x[E][W];
-  float m = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if (e * NT < nv) {
-      s.load((int64_t)e * NT + threadIdx.x, x[e]);
-    }
-  }
-  const Teacher tr = teacher_row<T, NT>(g, row, ent, red);
+  for (int e = 0; e < E; ++e)
+    if (e * NT < nv) s.load((int64_t)e * NT + threadIdx.x, x[e]);
+  // maxima of the row and of the teacher's scores together, then both sums of exponentials
+  float v[3] = {-INFINITY, 0.0f, 0.0f};
+  load_entries<T, NT>(g, row, ent, &v[1], &v[2]);
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (e * NT < nv) {
 #pragma unroll
-      for (int u = 0; u < W; ++u) m = fmaxf(m, x[e][u]);
+      for (int u = 0; u < W; ++u) v[0] = fmaxf(v[0], x[e][u]);
     }
-  m = all_max<NT>(m, red);
-  float sum = 0.0f;
+  all<NT, 3>(v, red, Max());
+  const float m = v[0];
+  float sums[2] = {0.0f, weigh_entries<NT>(g, ent, v[1])};
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (e * NT < nv) {
@@ -245,33 +285,39 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
       for (int u = 0; u < W; ++u) {
         // outside the row -inf gives 0, unless the whole row is -inf: NaN, as the definition has it
         x[e][u] = expf((x[e][u] - m) * g.inv_tau);
-        sum += x[e][u];
+        sums[0] += x[e][u];
       }
     }
-  sum = all_sum<NT>(sum, red);
-  const double lse = (double)m / g.tau + log((double)sum);
-  const float loss = row_loss<T, NT>(g, row, ent, tr, lse, redd);
-  if (threadIdx.x == 0) {
-    g.loss[row] = loss;
-    g.lse[row] = (float)lse;
-  }
-  if (!GRAD) return;
-  const float scale = row_scale(g, row, tr);
+  all<NT, 2>(sums, red, Add());  // (behind it every entry is in LDS)
+  if (NT == 64) __syncthreads();
+  const Teacher tr = teacher_of(v[1], v[2], sums[1]);
+  const float inv = 1.0f / sums[0];
+  const float scale = GRAD ? row_scale(g, row, tr.some, tr.bad) : 0.0f, by = scale * inv;
+  auto p_of = [&](int e) { return ent.w[e] * tr.inv; };
+  Writer<T, NT, decltype(p_of)> entries(g, ent, s.p, 0, g.V, p_of);
   T* o = static_cast<T*>(g.grad) + row * g.V;
-  const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
-  const float inv = 1.0f / sum, by = scale * inv;
+  if (GRAD) {
+    entries.look(threadIdx.x);
+    const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (e * NT < nv) {
+    for (int e = 0; e < E; ++e)
+      if (e * NT < nv) {
 #pragma unroll
-      for (int u = 0; u < W; ++u) x[e][u] = scale == 0.0f ? 0.0f : x[e][u] * by;
-      s.store(o, same, (int64_t)e * NT + threadIdx.x, x[e]);
-    }
-  if (scale == 0.0f) return;
+        for (int u = 0; u < W; ++u) x[e][u] = scale == 0.0f ? 0.0f : x[e][u] * by;
+        s.store(o, same, (int64_t)e * NT + threadIdx.x, x[e]);
+      }
+  }
   __syncthreads();
-  write_entries<T, NT>(g, row, ent, scale, 0, g.V, [&](int id) {
-    return expf((to_float<T>(s.p[id]) - m) * g.inv_tau) * inv;
-  });
+  if (GRAD && scale != 0.0f) entries.write(o, scale, [&](float v) { return expf((v - m) * g.inv_tau) * inv; });
+  if (threadIdx.x < 64) {
+    double terms, sum;
+    loss_terms<T>(g, row, ent, tr, &terms, &sum);
+    if (threadIdx.x == 0) {
+      const double lse = (double)m / g.tau + log((double)sums[0]);
+      g.loss[row] = loss_of(g, tr.some, tr.bad, terms, sum, lse);
+      g.lse[row] = (float)lse;
+    }
+  }
 }
 
 // ---- rows split along V ---------------------------------------------------------------------------------------------------
@@ -280,9 +326,20 @@ constexpr int kPartThreads = 256, kPartE = 8;
 template <typename T>
 __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
-  __shared__ float red[16];
-  const int64_t row = blockIdx.x / g.parts;
-  const int part = (int)(blockIdx.x % g.parts);
+  __shared__ float red[48];
+  __shared__ Entries ent;
+  const int64_t row = blockIdx.x / (g.parts + 1);
+  const int part = (int)(blockIdx.x % (g.parts + 1));
+  if (part == g.parts) {  // the row's teacher: what the second launch needs of it
+    const Teacher tr = teacher_row<T, NT>(g, row, ent, red);
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      double terms, all_p;
+      loss_terms<T>(g, row, ent, tr, &terms, &all_p);
+      if (threadIdx.x == 0) g.rec[row] = RowTeacher{tr.top, tr.inv, tr.some, tr.bad, terms, all_p};
+    }
+    return;
+  }
   const Row<T> s(g.logits, row, g.V);
   const int64_t first = part * g.span, last = min(s.vectors(), first + g.span);
   float x[kPartE][W];
@@ -298,25 +355,27 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   for (int e = 0; e < kPartE; ++e)
 #pragma unroll
     for (int u = 0; u < W; ++u) m = fmaxf(m, x[e][u]);
-  m = all_max<NT>(m, red);
-  float sum = 0.0f;
+  float top[1] = {m};
+  all<NT, 1>(top, red, Max());
+  m = top[0];
+  float sum[1] = {0.0f};
 #pragma unroll
   for (int e = 0; e < kPartE; ++e)
 #pragma unroll
-    for (int u = 0; u < W; ++u) sum += x[e][u] == -INFINITY ? 0.0f : expf((x[e][u] - m) * g.inv_tau);
-  sum = all_sum<NT>(sum, red);
-  if (threadIdx.x == 0) g.stat[row * g.parts + part] = make_float2(m, sum);
+    for (int u = 0; u < W; ++u) sum[0] += x[e][u] == -INFINITY ? 0.0f : expf((x[e][u] - m) * g.inv_tau);
+  all<NT, 1>(sum, red, Add());
+  if (threadIdx.x == 0) g.stat[row * g.parts + part] = make_float2(m, sum[0]);
 }
 
-// JOIN: from the parts' maxima and sums, part 0 writing loss and lse; otherwise from the lse that the caller kept
+// JOIN: from the parts' maxima and sums and the row's record, part 0 writing loss and lse; otherwise from the lse that the caller
+// kept
 template <typename T, bool JOIN, bool GRAD>
 __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int parts_here) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
-  __shared__ float red[16];
-  __shared__ double redd[16];
+  __shared__ float red[48];
   __shared__ Entries ent;
   const int64_t row = blockIdx.x / parts_here;
-  const int part = (int)(blockIdx.x % parts_here);
+  const int part = (int)(blockIdx.x % parts_here), lane = threadIdx.x & 63;
   const Row<T> s(g.logits, row, g.V);
   const int64_t first = part * g.span, last = min(s.vectors(), first + g.span);
   float x[kPartE][W];
@@ -327,35 +386,44 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
       if (i < last) s.load(i, x[e]);
     }
   }
-  const Teacher tr = teacher_row<T, NT>(g, row, ent, red);
+  Teacher tr;
   float m, inv;
   if (JOIN) {
+    // (every wavefront joins the parts for itself: no barrier to wait at)
+    const RowTeacher rec = g.rec[row];
+    tr.top = rec.top; tr.inv = rec.inv; tr.some = rec.some; tr.bad = rec.bad;
+    if (GRAD) {
+      float a, b;
+      load_entries<T, NT>(g, row, ent, &a, &b);
+    }
     m = -INFINITY;
-    for (int c = threadIdx.x; c < g.parts; c += NT) m = fmaxf(m, g.stat[row * g.parts + c].x);
-    m = all_max<NT>(m, red);
+    for (int c = lane; c < g.parts; c += 64) m = fmaxf(m, g.stat[row * g.parts + c].x);
+    m = across_wave(m, Max());
     float sum = 0.0f;
-    for (int c = threadIdx.x; c < g.parts; c += NT) {
+    for (int c = lane; c < g.parts; c += 64) {
       const float2 v = g.stat[row * g.parts + c];
       sum += v.y * expf((v.x - m) * g.inv_tau);  // a part of nothing but -inf adds 0, a row of nothing else gives NaN
     }
-    sum = all_sum<NT>(sum, red);
+    sum = across_wave(sum, Add());
     inv = 1.0f / sum;
-    if (part == 0) {
+    if (part == 0 && threadIdx.x == 0) {
       const double lse = (double)m / g.tau + log((double)sum);
-      const float loss = row_loss<T, NT>(g, row, ent, tr, lse, redd);
-      if (threadIdx.x == 0) {
-        g.loss[row] = loss;
-        g.lse[row] = (float)lse;
-      }
+      g.loss[row] = loss_of(g, tr.some, tr.bad, rec.terms, rec.sum, lse);
+      g.lse[row] = (float)lse;
     }
   } else {
+    tr = teacher_row<T, NT>(g, row, ent, red);
     m = g.lse_in[row] * g.tau;  // exp((s - tau lse) / tau) is q itself
     inv = 1.0f;
   }
   if (!GRAD) return;
-  const float scale = row_scale(g, row, tr), by = scale * inv;
+  const float scale = row_scale(g, row, tr.some, tr.bad), by = scale * inv;
   T* o = static_cast<T*>(g.grad) + row * g.V;
   const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
+  auto p_of = [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; };
+  Writer<T, NT, decltype(p_of)> entries(g, ent, s.p, first * W - s.off, last * W - s.off, p_of);
+  __syncthreads();  // (every entry is in LDS)
+  entries.look(threadIdx.x);
 #pragma unroll
   for (int e = 0; e < kPartE; ++e) {
     const int64_t i = first + (int64_t)e * NT + threadIdx.x;
@@ -367,9 +435,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
   }
   if (scale == 0.0f) return;
   __syncthreads();
-  write_entries<T, NT>(g, row, ent, scale, first * W - s.off, last * W - s.off, [&](int id) {
-    return expf((to_float<T>(s.p[id]) - m) * g.inv_tau) * inv;
-  });
+  entries.write(o, scale, [&](float v) { return expf((v - m) * g.inv_tau) * inv; });
 }
 
 // ---- which form a call takes ---------------------------------------------------------------------------------------------
@@ -405,7 +471,7 @@ void launch_forward(Args a, hipStream_t st) {
   const Split sp = split_of(a.R, a.V, W);
   a.parts = sp.parts;
   a.span = sp.span;
-  hipLaunchKernelGGL((k_distill_stats<T>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), 0, st, a);
+  hipLaunchKernelGGL((k_distill_stats<T>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), 0, st, a);
   const int here = GRAD ? sp.parts : 1;
   hipLaunchKernelGGL((k_distill_finish<T, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), 0, st, a, here);
 }
@@ -421,7 +487,7 @@ size_t need(int64_t R, int64_t V) {
   size_t most = 0;
   for (int W : {4, 8})
     if (!in_registers(R, V, W)) {
-      const size_t n = (size_t)R * split_of(R, V, W).parts * sizeof(float2);
+      const size_t n = (size_t)R * (sizeof(RowTeacher) + split_of(R, V, W).parts * sizeof(float2));
       if (n > most) most = n;
     }
   return (most + 255) / 256 * 256;
@@ -492,7 +558,7 @@ int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, cons
   if (rows == 0) return SPCFG_OK;
   if (!loss || !lse) return SPCFG_ERR_ARG;
   if ((rc = check_workspace(rows, V, workspace, workspace_bytes))) return rc;
-  a.loss = loss; a.lse = lse; a.stat = static_cast<float2*>(workspace);
+  a.loss = loss; a.lse = lse; a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
   if (type == SPCFG_TYPE_F32) launch_forward<float, false>(a, (hipStream_t)hip_stream);
   else launch_forward<uint16_t, false>(a, (hipStream_t)hip_stream);
   return launch_status();
@@ -525,7 +591,7 @@ int spcfg_distill_forward_backward(int32_t type, int32_t rows, int32_t V, int32_
   a.grad_loss = grad_loss; a.grad = grad_logits;
   if ((rc = check_grad(type, a, grad_logits))) return rc;
   if ((rc = check_workspace(rows, V, workspace, workspace_bytes))) return rc;
-  a.loss = loss; a.lse = lse; a.stat = static_cast<float2*>(workspace);
+  a.loss = loss; a.lse = lse; a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
   if (type == SPCFG_TYPE_F32) launch_forward<float, true>(a, (hipStream_t)hip_stream);
   else launch_forward<uint16_t, true>(a, (hipStream_t)hip_stream);
   return launch_status();
