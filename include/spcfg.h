@@ -232,8 +232,10 @@ int spcfg_rules_backward(int32_t N, int32_t P, int32_t V, const float* log_root,
  *   x dev [rows x in], W dev [out x in], bias dev [out] or NULL, residual dev [rows x out] or NULL, y dev [rows x out]
  * x, W, bias and the gradients of all three have in_type; y, residual, preact and grad_y have out_type.  All matrices are
  * row-major and dense; their pointers need no more than the alignment of one element (16-byte alignment of rows is faster).
- *   in_type F32 (out_type F32): operands are cut exactly into three bf16 pieces and six piece products accumulated in fp32,
- *     as accurate as an fp32 product.  An infinite operand (or one above 3.38e38, which rounds to an infinite piece) gives NaN.
+ *   in_type F32 (out_type F32): products of 16-bit pieces of the operands, accumulated in fp32, with the accuracy of an fp32
+ *     product: three exact bf16 pieces of each value, or, in large forward products, two fp16 pieces of its row scaled by a
+ *     power of two (values below 2^-29 of their row's largest are then good to 2^-51 of that one).  An infinite operand makes
+ *     the results that it enters NaN, and one above 3.38e38 may.
  *   in_type BF16 (out_type BF16 or F32): products of the given values accumulated in fp32; the backward pass rounds
  *     grad_y * act'(z) to bf16, the operands' type.
  * Activations and epilogues are computed in fp32 and rounded to the result's type once.
@@ -261,7 +263,8 @@ int spcfg_dense_workspace_bytes(const spcfg_dense_config* cfg, size_t* out_bytes
 
 /*
  *   preact     dev [rows x out] or NULL: z, for the backward pass (only needed with an activation)
- *   workspace  dev, 256-byte aligned, >= spcfg_dense_workspace_bytes(...) bytes; holds nothing between calls
+ *   workspace  dev, 256-byte aligned, >= spcfg_dense_workspace_bytes(...) bytes; holds nothing between calls.  Calls and
+ *              replays of captured ones that may overlap need workspaces of their own
  * residual may be x (where the types and sizes allow it) and y may be residual; outputs overlap nothing else.
  */
 int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void* W, const void* bias, const void* residual,
@@ -294,7 +297,8 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
  *   grad_loss      dev [rows] float or NULL (= all ones): what each row's loss counts in the sum that is differentiated
  *   grad_logits    dev [rows x V] of `type`: grad_loss * temperature * (q_j - sum of the p_e with id(e) = j); overwritten,
  *                  overlaps nothing else
- *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted)
+ *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted); holds
+ *                  nothing between calls, calls that may overlap need their own
  * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An id >= V gives the row's loss and
  * gradient NaN, and so does a NaN among its scores; a student's score of -inf where p > 0 gives an infinite loss and a
  * finite gradient.  Matrices are dense, pointers need the alignment of one element.  rows may be 0; rows <= 2^20,
@@ -326,8 +330,8 @@ int spcfg_distill_forward_backward(int32_t type, int32_t rows, int32_t V, int32_
  *   grad_loss        dev [pairs] or NULL (= all ones)
  *   grad_logZ        dev [B]: gradient of sum_p grad_loss[p] * loss[p]; overwritten, 0 for sentences without pairs
  * A pair with a negative index is absent, and so is one whose margin is a difference of equal infinities (no grammar derives
- * either sentence): loss, margin and gradient 0.  An index >= B gives loss and margin NaN, and NaN as the gradient of the pair's other
- * sentence.  Outputs overlap nothing else.  1 <= B <= 65536, 0 <= pairs <= 2^20.  Deterministic; the gradient's cost
+ * either sentence): loss, margin and gradient 0.  An index >= B gives loss and margin NaN, and NaN as the gradient of the
+ * pair's other sentence.  Outputs overlap nothing else.  1 <= B <= 65536, 0 <= pairs <= 2^20.  Deterministic; the gradient's cost
  * grows with B * pairs.
  */
 int spcfg_preference_forward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,

@@ -220,8 +220,8 @@ __global__ void __launch_bounds__(64 * kWaves) k_dense_backward(Args g, unsigned
 
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
 
-// Tiles of 16 where there are few of 32, or no more than 16 rows (us on 16 / 32: fp32 30 x 512 x 512 4.8 / 7.7, 333 x 141 x 474 7.9 / 6.2,
-// backward 11.6 / 15.4, 200 x 512 x 512 backward 15.7 / 11, 1 x 512 x 10000 8.9 / 10.5).
+// Tiles of 16 where there are few of 32, or no more than 16 rows (us on 16 / 32: fp32 30 x 512 x 512 4.8 / 7.7,
+// 333 x 141 x 474 7.9 / 6.2, backward 11.6 / 15.4, 200 x 512 x 512 backward 15.7 / 11, 1 x 512 x 10000 8.9 / 10.5).
 constexpr int kFew = 160;
 
 template <typename TI, typename TO, int T>

@@ -13,13 +13,15 @@
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
 //    32 or 64 values of k: rows of 64 or 128 bytes along k, with the 16-byte piece XORed with bits 2..3, resp. 1..3 of the
-//    row; across k rows of 128 or 64 columns, with the 64-byte piece XORed with the row mod 4, resp. bit 1 of it.  Operands come out of LDS with
-//    ds_read_b128, resp. with the transposing ds_read_b64_tr_b16; both forms meet no bank conflict.
+//    row; across k rows of 128 or 64 columns, with the 64-byte piece XORed with the row mod 4, resp. bit 1 of it.  Operands
+//    come out of LDS with ds_read_b128, resp. with the transposing ds_read_b64_tr_b16.
 //  * The order of a step is written out: products of 16 k while the next 16 are read; behind the first products of the last 16
 //    the barrier - each wavefront's loads of the next step have landed, nobody needs this step's tiles any more - then the
 //    next step's first operands are read and this step's place is filled with the tiles of step + NS.
 //  * Few tiles: k is split over workgroups, which leave fp32 partial tiles; a second launch adds them in order.
-// No launch waits for another workgroup; sums run in an order fixed by the sizes.
+// No workgroup waits for another; sums run in an order fixed by the sizes.
+// Bound by the matrix cores on wide layers (bf16 8192^3 1250 TFLOP/s, 8192 x 4096 x 4096 with gelu 241 to 250 us = 1100 to 1140;
+// a library product of that size 1297), by LDS reads on tiles of 128 (700 to 800 TFLOP/s), by latency below some 2e9 products.
 #include <type_traits>
 #include <utility>
 
@@ -136,7 +138,8 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   const unsigned lds0 = lds_address(lds);
   unsigned e_off[ND], e_lds[ND];
   constexpr int RL = 1024 / S::RB;                               // rows of a load along k
-  constexpr int PW = S::BM < 128 ? 64 : 128, RP = 512 / PW, QA = ME / RP;  // across: columns of a panel, rows of a load, loads of a panel
+  // across: columns of a panel, rows of a load, loads of a panel
+  constexpr int PW = S::BM < 128 ? 64 : 128, RP = 512 / PW, QA = ME / RP;
   // row of those, and piece: XOR with bits of the row (the loads of a plane are RL rows apart, a multiple of 8)
   const int r_al = lane / (64 / RL), c_al = (lane & (64 / RL - 1)) ^ (ME == 32 ? (r_al >> 2) & 3 : 0);
   const int r_ac = lane / (64 / RP), key_ac = PW == 128 ? r_ac & 3 : (r_ac >> 1) & 1;
@@ -438,7 +441,8 @@ __global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>()) k_dense_forwa
 // Both products of the backward pass and the bias's gradient in one launch: the CUs that one leaves idle are the other's.  Each
 // part's workgroups start at a multiple of 8, so that the XCD is the same function of either index.
 template <typename S, typename TI, typename TO>
-__global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>()) k_dense_backward_tiles(Args g, Product px, Product pw, const float* sums, int parts) {
+__global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>())
+    k_dense_backward_tiles(Args g, Product px, Product pw, const float* sums, int parts) {
   __shared__ __align__(1024) unsigned char lds[S::kLds];
   unsigned b = blockIdx.x;
   const unsigned room_x = (px.wgs + 7) / 8 * 8, room_w = (pw.wgs + 7) / 8 * 8;
@@ -499,7 +503,8 @@ __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t, const float (
 // eight values of a row from column c on, zero outside the matrix (where the nearest ones inside are loaded: no load hangs on a
 // branch of its own)
 template <typename T>
-__device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, bool vec, float (&v)[8]) {
+__device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, bool vec,
+                                      float (&v)[8]) {
   T x[8];
   const T* row = src + min(r, rows - 1) * cols;
   if (vec) {  // (cols is a multiple of 8)
@@ -577,7 +582,8 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
   if (wave == 0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < g.O) sums[(int64_t)part * g.O + c + i] = ((s[i] + red[0][lane * 8 + i]) + red[1][lane * 8 + i]) + red[2][lane * 8 + i];
+      if (c + i < g.O)
+        sums[(int64_t)part * g.O + c + i] = ((s[i] + red[0][lane * 8 + i]) + red[1][lane * 8 + i]) + red[2][lane * 8 + i];
   }
 }
 
@@ -675,20 +681,24 @@ struct Choice { int t, sa, sb; double us; };
 
 // Into how many workgroups each tile's steps are cut, for two products of one launch (or one, the other of no size), with one
 // tiling.  A step takes what it takes alone or its share of the CU, whichever is longer; the launch is estimated as the longest
-// workgroup where all run at once, as their mean with half the longest on top where they do not; splitting costs a launch more (6 us) and partial tiles written and read
-// again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
+// workgroup where all run at once, as their mean with half the longest on top where they do not; splitting costs a launch
+// more (6 us) and partial tiles written and read again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
 // Measured (us): 4096 x 512 x 512 in fp32 (128 tiles of 128 x 128, 16 steps) in two 37, in one 30, on 64 x 64 24;
 // bf16 8192 x 4096 x 4096 on 256 x 256 241, on 128 x 128 320; 2048 x 512 x 10000 61, 43; 512^3 on 128 x 128 9.7, on 64 x 64 6.9.
 void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Choice* best) {
-  auto work = [&](const int64_t (&d)[3]) { return Work{d[2] ? tiles(d[0], g.t) * tiles(d[1], g.t) : 0, tiles(d[2], g.bk)}; };
+  auto work = [&](const int64_t (&d)[3]) {
+    return Work{d[2] ? tiles(d[0], g.t) * tiles(d[1], g.t) : 0, tiles(d[2], g.bk)};
+  };
   const Work wa = work(a), wb = work(b);
   const int64_t longer = wb.steps > wa.steps ? wb.steps : wa.steps;
   for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
     if (s > 1 && longer < (int64_t)s * g.least) break;
-    const int64_t len = tiles(longer, s), pa = wa.n ? tiles(wa.steps, (int)len) : 0, pb = wb.n ? tiles(wb.steps, (int)len) : 0;
+    const int64_t len = tiles(longer, s), pa = wa.n ? tiles(wa.steps, (int)len) : 0;
+    const int64_t pb = wb.n ? tiles(wb.steps, (int)len) : 0;
     const double wgs = (double)(wa.n * pa + wb.n * pb), here = (wgs < g.room ? wgs : g.room) / 256;
     const double step = here * g.busy > g.wait ? here * g.busy : g.wait;
-    const double ta = pa ? g.start + step * tiles(wa.steps, (int)pa) : 0, tb = pb ? g.start + step * tiles(wb.steps, (int)pb) : 0;
+    const double ta = pa ? g.start + step * tiles(wa.steps, (int)pa) : 0;
+    const double tb = pb ? g.start + step * tiles(wb.steps, (int)pb) : 0;
     const double most = ta > tb ? ta : tb, mean = (wa.n * pa * ta + wb.n * pb * tb) / g.room;
     double us = wgs <= g.room ? most : mean + 0.5 * most;
     if (us < most) us = most;
@@ -743,7 +753,8 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   // beside the products: a launch for planes and dz, 3 us and its bytes at 4 TB/s
   const double si = fp32 ? 4 : 2, so = out_type == SPCFG_TYPE_F32 ? 4 : 2;
   double bytes = 0;
-  if (p.cut) bytes += (what != BACK_X ? (double)R * I : 0) * (fp32 && what == FORWARD ? 8 : si * 2.5) + (what != BACK_W ? (double)O * I : 0) * (fp32 && what == FORWARD ? 8 : si * 2.5);
+  const double a_value = fp32 && what == FORWARD ? 8 : si * 2.5;
+  if (p.cut) bytes += a_value * ((what != BACK_X ? (double)R * I : 0) + (what != BACK_W ? (double)O * I : 0));
   if (what != FORWARD) bytes += (double)R * O * ((act ? 2 : 1) * so + (p.dz ? 2 * pl : 0));
   const double us = p.c.us + (bytes > 0 ? 3 + bytes / 4e6 : 0);
   p.on = us < direct_us(R, I, O, in_type, what);

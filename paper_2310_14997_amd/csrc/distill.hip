@@ -4,8 +4,10 @@
 //   loss = tau^2 sum_e p_e (log p_e - log q_id(e)),         d loss / d s_j = tau (q_j - sum_{e: id(e) = j} p_e)
 // Bound by HBM: the row is read once and its gradient written once.  A row that a workgroup can hold in registers is one
 // pass; longer rows, and few rows, are split over workgroups along V: one launch leaves each part's maximum and sum of
-// exponentials (and, once a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p are in 32 bits; logarithms and the
-// sum over the teacher's entries, whose terms cancel where q is near p, in 64.
+// exponentials (and, once a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p
+// are in 32 bits; logarithms and the sum over the teacher's entries, whose terms cancel where q is near p, in 64.
+// 2048 rows of 10000 floats, k = 64: 37 us (4.4 TB/s; a copy of that size 30).  8 rows of 131071 bf16, k = 128: 8 + 10 us, two
+// latencies.  512 threads a row instead of 256 were no faster, 1024 twice as slow.
 #include <cmath>
 
 #include "spcfg_internal.h"
@@ -179,7 +181,8 @@ __device__ __forceinline__ Teacher teacher_row(const Args& g, int64_t row, Entri
 
 // One wavefront: sum of p (log p - s / tau) and of p over the row's entries, in 64 bits.  E is complete (behind a barrier).
 template <typename T>
-__device__ __forceinline__ void loss_terms(const Args& g, int64_t row, const Entries& E, const Teacher& tr, double* terms, double* sum) {
+__device__ __forceinline__ void loss_terms(const Args& g, int64_t row, const Entries& E, const Teacher& tr, double* terms,
+                                           double* sum) {
   const T* t = static_cast<const T*>(g.teacher) + row * g.k;
   const T* s = static_cast<const T*>(g.logits) + row * g.V;
   const double inv_tau = 1.0 / g.tau, top = tr.top * inv_tau, log_inv = log((double)tr.inv);
