@@ -364,11 +364,13 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 
   // Epilogue: 32 rows of a wavefront at a time go through its own part of LDS, from the accumulators' order (32 x 32 tile: column
   // lane % 32, row 8 (v / 4) + 4 (lane / 32) + v % 4) to eight adjacent columns a lane.  Rows there are 32 NI + 8 floats
-  // apart: the two halves of a wavefront write rows four apart, in different banks.
+  // apart: the two halves of a wavefront write rows four apart, in different banks; groups of four columns change places in
+  // odd rows, so that the reads of adjacent rows are in different banks too.
   constexpr int LR = 32 * NI + 8, PER_ROW = 4 * NI, ROWS = 64 / PER_ROW;  // lanes of a row, rows at a time
   static_assert(S::NW * 32 * LR * 4 <= S::kLds, "the epilogue's rows fit");
   __syncthreads();  // (nobody reads operands any more)
   float* out = reinterpret_cast<float*>(lds) + wave * 32 * LR;
+  const int odd = lane / PER_ROW % 2 * 4;
   const int64_t mw = m0 + wm * MI * 32 + lane / PER_ROW, c = n0 + wn * NI * 32 + lane % PER_ROW * 8;
   const Epilogue<TI, TO, FORM> ep(g, p.N);
   float* part = p.splits > 1 ? p.partial + (int64_t)split * p.M * p.N : nullptr;
@@ -387,7 +389,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     constexpr int mi = decltype(i)::value;
     static_for<0, 16 * NI>([&](auto w) {
       constexpr int v = decltype(w)::value / NI, ni = decltype(w)::value % NI;
-      out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * LR + ni * 32 + (lane & 31)] = total(mi, ni, v);
+      out[(8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * LR + ((ni * 32 + (lane & 31)) ^ ((v & 1) * 4))] = total(mi, ni, v);
     });
     // (a wavefront's own accesses to LDS are in order; the fences keep the compiler's)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -396,7 +398,10 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       const float* from = out + (r + lane / PER_ROW) * LR + lane % PER_ROW * 8;
       float s[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s[u] = from[u];
+      for (int u = 0; u < 4; ++u) {
+        s[u] = from[odd + u];
+        s[u + 4] = from[4 - odd + u];
+      }
       if (m >= p.M || c >= p.N) continue;
       if (PL == 2) {
         const int e = p.exp_a[m];
