@@ -133,7 +133,7 @@ def test_backward(R, I, O, types):
 
 # sizes of more work: whole and ragged tiles along each side, long sums with few rows, few columns, few inputs
 LARGE = [(2048, 512, 512), (1025, 264, 1111), (130, 2050, 700), (4100, 72, 130), (96, 1024, 6000), (2500, 640, 40),
-         (777, 333, 1999)]
+         (777, 333, 1999), (2050, 520, 4104), (100, 4000, 1000), (8200, 512, 512)]
 
 
 @pytest.mark.parametrize("types", TYPES, ids="-".join)
@@ -324,3 +324,57 @@ def test_streams_and_graphs(R, I, O):
         bwd()
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(outs, got)), turn
+
+
+def test_matrices_of_more_than_32_bits_of_bytes():
+    """y, z and grad_y of 4.6 GB each: the last rows, and gradients that all rows add up to; references in 64 bits on the GPU."""
+    import torch
+    R, I, O = 140001, 64, 16392
+    print("case dense far offsets", R, I, O, flush=True)
+    b16, dev = torch.bfloat16, "cuda:0"
+    g = torch.Generator(device=dev)
+    g.manual_seed(3)
+    n = lambda *s: torch.randn(*s, generator=g, device=dev)
+    x, W, b = n(R, I).to(b16), (0.2 * n(O, I)).to(b16), n(O).to(b16)
+    cfg = bd.make_dense_config(R, I, O, bd.TYPE_BF16, bd.TYPE_BF16, bd.ACT_RELU)
+    ws = workspace(cfg)
+    y, z = torch.empty(R, O, dtype=b16, device=dev), torch.empty(R, O, dtype=b16, device=dev)
+    bd.spcfg_dense_forward(cfg, x, W, b, None, y, z, ws)
+    D = lambda t: t.double()
+    rows = torch.cat([torch.arange(3), torch.arange(R // 2, R // 2 + 3), torch.arange(R - 5, R)]).to(dev)
+    want = D(x[rows]) @ D(W).t() + D(b)
+    q = torch.sqrt((D(x[rows]) ** 2) @ (D(W) ** 2).t())
+    tol = U * (16 + 6 * I / 16) * 2 * q + (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -20
+    close("preact", values(z[rows]), want.cpu().numpy(), tol.cpu().numpy())
+    close("y", values(y[rows]), want.clamp(min=0).cpu().numpy(), tol.cpu().numpy())
+    gy = y  # (its own buffer as an upstream gradient: any values do)
+    gx, gW, gb = torch.empty(R, I, dtype=b16, device=dev), torch.empty(O, I, dtype=b16, device=dev), torch.empty(O, dtype=b16, device=dev)
+    bd.spcfg_dense_backward(cfg, x, W, z, gy, None, gx, gW, gb, ws)
+    cols = torch.tensor([0, 1, O // 2, O - 2, O - 1], device=dev)
+    for name, got, A, B, K in (("grad_x", gx[rows], D(gy[rows]) * (D(z[rows]) > 0), D(W), O),
+                               ("grad_W", gW[cols], (D(gy[:, cols]) * (D(z[:, cols]) > 0)).t(), D(x), R)):
+        want, q = A @ B, torch.sqrt((A ** 2) @ (B ** 2))
+        tol = (U * (16 + 6 * K / 16) * 2 + 4 * 2.0 ** -8) * q + (2.0 ** -8 + 2.0 ** -22) * want.abs()
+        close(name, values(got), want.cpu().numpy(), tol.cpu().numpy())
+    want = (D(gy[:, cols]) * (D(z[:, cols]) > 0)).sum(0)
+    # (terms of one sign: every addition rounds a sum as large as the result, 16 rows in a row, then parts of the rows)
+    close("grad_bias", values(gb[cols]), want.cpu().numpy(), ((2.0 ** -8 + 2.0 ** -15) * want.abs()).cpu().numpy())
+
+
+def test_the_binding_refuses_other_tensors():
+    import torch
+    e = lambda *s, **k: torch.empty(*s, device="cuda:0", **k)
+    cfg = bd.make_dense_config(4, 8, 6)
+    ok = dict(x=e(4, 8), W=e(6, 8), bias=e(6), residual=None, y=e(4, 6), preact=None, workspace=None)
+    for bad, what in ((dict(x=e(4, 7)), ValueError), (dict(W=e(8, 6).t()), TypeError), (dict(bias=e(6, dtype=torch.float64)), TypeError),
+                      (dict(y=torch.empty(4, 6)), TypeError), (dict(residual=e(4, 8)), ValueError), (dict(x=[1.0]), TypeError),
+                      (dict(workspace=e(64)), TypeError)):
+        with pytest.raises(what):
+            bd.spcfg_dense_forward(cfg, **{**ok, **bad})
+    with pytest.raises(bd.SpcfgError) as err:
+        bd.spcfg_dense_forward(bd.make_dense_config(4, 8, 6, 5, 0), **ok)
+    assert err.value.code == -5
+    big = bd.make_dense_config(2048, 512, 2048)
+    with pytest.raises(bd.SpcfgError) as err:
+        bd.spcfg_dense_forward(big, e(2048, 512), e(2048, 512), None, None, e(2048, 2048), None, None)
+    assert err.value.code == -1

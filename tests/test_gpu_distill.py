@@ -191,3 +191,28 @@ def test_no_rows_and_graphs():
             step()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, (l, e, gr))), (R, V, turn)
+
+
+def test_tables_of_more_than_32_bits_of_bytes():
+    """Rows past 4 GB and 2^31 elements, in a table of 5.4 GB: the last rows against the oracle, the others by what they add up to."""
+    import torch
+    for R, V in ((20600, 131072), (131090, 20480)):
+        print("case distill far offsets", R, V, flush=True)
+        dev, b16, k = "cuda:0", torch.bfloat16, 7
+        g = torch.Generator(device=dev)
+        g.manual_seed(R)
+        s = torch.empty(R, V, dtype=b16, device=dev)
+        for r in range(0, R, 4096):
+            s[r:r + 4096] = torch.randn(min(4096, R - r), V, generator=g, device=dev).to(b16)
+        t = torch.randn(R, k, generator=g, device=dev).to(b16)
+        ids = torch.randint(0, V, (R, k), generator=g, device=dev, dtype=torch.int32)
+        l, e, gr = torch.empty(R, device=dev), torch.empty(R, device=dev), torch.empty_like(s)
+        bd.spcfg_distill_forward_backward(s, t, ids, 1.0, None, l, e, gr, scratch(R, V))
+        pick = torch.tensor([0, 1, R // 2, R - 2, R - 1], device=dev)
+        loss, lse, grad = LO.distill(values(s[pick]), values(t[pick]), ids[pick].cpu().numpy(), 1.0)
+        close("loss", values(l[pick]), loss, 2.0 ** -19 + 2.0 ** -17 * np.abs(loss))
+        close("lse", values(e[pick]), lse, 2.0 ** -19 + 2.0 ** -23 * np.abs(lse))
+        close("gradient", values(gr[pick]), grad, 2.0 ** -8 * np.abs(grad) + 2.0 ** -18 * np.exp(values(s[pick]) - lse[:, None]) + 2.0 ** -20 * (grad < 0))
+        bd.spcfg_distill_backward(s, t, ids, 1.0, e, None, gr)
+        close("gradient from lse", values(gr[pick]), grad, (2.0 ** -8 + 2.0 ** -16) * np.abs(grad) + 2.0 ** -16 * np.exp(values(s[pick]) - lse[:, None]) + 2.0 ** -20 * (grad < 0))
+        del s, gr
