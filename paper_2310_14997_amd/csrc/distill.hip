@@ -203,25 +203,25 @@ __device__ __forceinline__ float loss_of(const Args& g, bool some, bool bad, dou
 }
 
 // Gradient entries that the teacher has, for ids in [lo, hi): the first of equal ids writes what all of them add up to, in
-// their order.  What each thread's first entry takes - its score, and a look at all ids for equal ones - is done ahead
-// (look), while the rest of the row is under way; write comes when the other entries have been written, behind a barrier.
-template <typename T, int NT, typename P> struct Writer {
+// their order.  A thread's first entry is looked at ahead (look: its score is asked for, all ids are looked through for equal
+// ones), while the rest of the row is under way; write comes when the other entries have been written, behind a barrier.
+template <typename T, int NT> struct Writer {
   const Args& g;
   const Entries& E;
   const T* s;
   int64_t lo, hi;
-  P p_of;               // p of entry e
-  float score, p;
-  bool first;
-  __device__ __forceinline__ Writer(const Args& g_, const Entries& E_, const T* s_, int64_t lo_, int64_t hi_, P p_of_)
-      : g(g_), E(E_), s(s_), lo(lo_), hi(hi_), p_of(p_of_) {}
+  T score;
+  bool first, behind;
+  __device__ __forceinline__ Writer(const Args& g_, const Entries& E_, const T* s_, int64_t lo_, int64_t hi_)
+      : g(g_), E(E_), s(s_), lo(lo_), hi(hi_) {}
   __device__ __forceinline__ void look(int e) {
     const int id = e < g.k ? E.id[e] : -1;
     first = id >= 0 && id >= lo && id < hi;
     if (!__any(first)) return;
-    if (first) score = to_float<T>(s[id]);
+    if (first) score = s[id];
     // equal ids: any before this one, any behind it (four at a time; from k on there is no id)
-    bool before = false, behind = false;
+    bool before = false;
+    behind = false;
 #pragma unroll 4
     for (int f = 0; f < g.k; f += 4) {
       const int4 at = *reinterpret_cast<const int4*>(&E.id[f]);
@@ -233,27 +233,28 @@ template <typename T, int NT, typename P> struct Writer {
       }
     }
     first = first && !before;
-    if (!first) return;
-    p = p_of(e);
-    if (behind) {
-      for (int f = e + 1; f < g.k; ++f)
-        if (E.id[f] == id) p += p_of(f);
-    }
   }
-  // q_of(score): the softmax's entry
-  template <typename Q> __device__ __forceinline__ void write(T* o, float scale, Q q_of) {
+  // q_of(score): the softmax's entry; p_of(e): p of entry e
+  template <typename Q, typename P> __device__ __forceinline__ void write(T* o, float scale, Q q_of, P p_of) {
     for (int e = threadIdx.x; e < g.k; e += NT) {
       if (e >= NT) look(e);
-      if (first) o[E.id[e]] = from_float<T>(scale * (q_of(score) - p));
+      if (!first) continue;
+      const int id = E.id[e];
+      float p = p_of(e);
+      if (behind) {
+        for (int f = e + 1; f < g.k; ++f)
+          if (E.id[f] == id) p += p_of(f);
+      }
+      o[id] = from_float<T>(scale * (q_of(to_float<T>(score)) - p));
     }
   }
 };
 
-// what the gradient of a row is scaled by; 0: the row is all zeros
-__device__ __forceinline__ float row_scale(const Args& g, int64_t row, bool some, bool bad) {
-  const float w = g.grad_loss ? g.grad_loss[row] : 1.0f;
-  if (w == 0.0f || !some) return 0.0f;
-  return bad ? NAN : w * g.tau;
+// what the row's loss counts, and what its gradient is scaled by; 0: the row is all zeros
+__device__ __forceinline__ float row_weight(const Args& g, int64_t row) { return g.grad_loss ? g.grad_loss[row] : 1.0f; }
+__device__ __forceinline__ float row_scale(const Args& g, float weight, bool some, bool bad) {
+  if (weight == 0.0f || !some) return 0.0f;
+  return bad ? NAN : weight * g.tau;
 }
 
 // ---- a row per workgroup, in registers ----------------------------------------------------------------------------------
@@ -265,6 +266,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   const int64_t row = blockIdx.x;
   const Row<T> s(g.logits, row, g.V);
   const int64_t nv = s.vectors();
+  const float weight = GRAD ? row_weight(g, row) : 0.0f;
   float x[E][W];
 #pragma unroll
   for (int e = 0; e < E; ++e)
@@ -278,7 +280,10 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
 #pragma unroll
       for (int u = 0; u < W; ++u) v[0] = fmaxf(v[0], x[e][u]);
     }
-  all<NT, 3>(v, red, Max());
+  all<NT, 3>(v, red, Max());  // (behind it every entry's id is in LDS)
+  if (NT == 64) __syncthreads();
+  Writer<T, NT> entries(g, ent, s.p, 0, g.V);
+  if (GRAD) entries.look(threadIdx.x);
   const float m = v[0];
   float sums[2] = {0.0f, weigh_entries<NT>(g, ent, v[1])};
 #pragma unroll
@@ -291,16 +296,12 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
         sums[0] += x[e][u];
       }
     }
-  all<NT, 2>(sums, red, Add());  // (behind it every entry is in LDS)
-  if (NT == 64) __syncthreads();
+  all<NT, 2>(sums, red, Add());
   const Teacher tr = teacher_of(v[1], v[2], sums[1]);
   const float inv = 1.0f / sums[0];
-  const float scale = GRAD ? row_scale(g, row, tr.some, tr.bad) : 0.0f, by = scale * inv;
-  auto p_of = [&](int e) { return ent.w[e] * tr.inv; };
-  Writer<T, NT, decltype(p_of)> entries(g, ent, s.p, 0, g.V, p_of);
+  const float scale = GRAD ? row_scale(g, weight, tr.some, tr.bad) : 0.0f, by = scale * inv;
   T* o = static_cast<T*>(g.grad) + row * g.V;
   if (GRAD) {
-    entries.look(threadIdx.x);
     const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -311,7 +312,9 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
       }
   }
   __syncthreads();
-  if (GRAD && scale != 0.0f) entries.write(o, scale, [&](float v) { return expf((v - m) * g.inv_tau) * inv; });
+  if (GRAD && scale != 0.0f) {
+    entries.write(o, scale, [&](float a) { return expf((a - m) * g.inv_tau) * inv; }, [&](int e) { return ent.w[e] * tr.inv; });
+  }
   if (threadIdx.x < 64) {
     double terms, sum;
     loss_terms<T>(g, row, ent, tr, &terms, &sum);
@@ -389,6 +392,8 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
       if (i < last) s.load(i, x[e]);
     }
   }
+  const float weight = GRAD ? row_weight(g, row) : 0.0f;
+  Writer<T, NT> entries(g, ent, s.p, first * W - s.off, last * W - s.off);
   Teacher tr;
   float m, inv;
   if (JOIN) {
@@ -398,6 +403,8 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     if (GRAD) {
       float a, b;
       load_entries<T, NT>(g, row, ent, &a, &b);
+      __syncthreads();
+      entries.look(threadIdx.x);
     }
     m = -INFINITY;
     for (int c = lane; c < g.parts; c += 64) m = fmaxf(m, g.stat[row * g.parts + c].x);
@@ -420,13 +427,13 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     inv = 1.0f;
   }
   if (!GRAD) return;
-  const float scale = row_scale(g, row, tr.some, tr.bad), by = scale * inv;
+  if (!JOIN) {
+    __syncthreads();
+    entries.look(threadIdx.x);
+  }
+  const float scale = row_scale(g, weight, tr.some, tr.bad), by = scale * inv;
   T* o = static_cast<T*>(g.grad) + row * g.V;
   const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
-  auto p_of = [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; };
-  Writer<T, NT, decltype(p_of)> entries(g, ent, s.p, first * W - s.off, last * W - s.off, p_of);
-  __syncthreads();  // (every entry is in LDS)
-  entries.look(threadIdx.x);
 #pragma unroll
   for (int e = 0; e < kPartE; ++e) {
     const int64_t i = first + (int64_t)e * NT + threadIdx.x;
@@ -438,7 +445,8 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
   }
   if (scale == 0.0f) return;
   __syncthreads();
-  entries.write(o, scale, [&](float v) { return expf((v - m) * g.inv_tau) * inv; });
+  entries.write(o, scale, [&](float a) { return expf((a - m) * g.inv_tau) * inv; },
+                [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; });
 }
 
 // ---- which form a call takes ---------------------------------------------------------------------------------------------
