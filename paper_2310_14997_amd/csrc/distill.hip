@@ -6,9 +6,10 @@
 // pass; longer rows, and few rows, are split over workgroups along V: one launch leaves each part's maximum and sum of
 // exponentials (and, once a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p
 // are in 32 bits; logarithms and the sum over the teacher's entries, whose terms cancel where q is near p, in 64.
-// 2048 rows of 10000 floats, k = 64: 37 us (4.4 TB/s; a copy of that size 30).  8 rows of 131071 bf16, k = 128: 8 + 10 us, two
-// latencies.  512 threads a row instead of 256 were no faster, 1024 twice as slow.
+// 2048 rows of 10000 floats, k = 64: 37 us (4.4 TB/s; a copy of that size 30).  8 rows of 131071 bf16, k = 128: 14 us, two
+// latencies.
 #include <cmath>
+#include <type_traits>
 
 #include "spcfg_internal.h"
 
@@ -327,9 +328,10 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
 }
 
 // ---- rows split along V ---------------------------------------------------------------------------------------------------
-constexpr int kPartThreads = 256, kPartE = 8;
+constexpr int kPartThreads = 256;
 
-template <typename T>
+// E: vectors of a thread
+template <typename T, int E>
 __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
   __shared__ float red[48];
@@ -348,17 +350,17 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   }
   const Row<T> s(g.logits, row, g.V);
   const int64_t first = part * g.span, last = min(s.vectors(), first + g.span);
-  float x[kPartE][W];
+  float x[E][W];
   float m = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < kPartE; ++e) {
+  for (int e = 0; e < E; ++e) {
     const int64_t i = first + (int64_t)e * NT + threadIdx.x;
 #pragma unroll
     for (int u = 0; u < W; ++u) x[e][u] = -INFINITY;
     if (i < last) s.load(i, x[e]);
   }
 #pragma unroll
-  for (int e = 0; e < kPartE; ++e)
+  for (int e = 0; e < E; ++e)
 #pragma unroll
     for (int u = 0; u < W; ++u) m = fmaxf(m, x[e][u]);
   float top[1] = {m};
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   m = top[0];
   float sum[1] = {0.0f};
 #pragma unroll
-  for (int e = 0; e < kPartE; ++e)
+  for (int e = 0; e < E; ++e)
 #pragma unroll
     for (int u = 0; u < W; ++u) sum[0] += x[e][u] == -INFINITY ? 0.0f : expf((x[e][u] - m) * g.inv_tau);
   all<NT, 1>(sum, red, Add());
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
 
 // JOIN: from the parts' maxima and sums and the row's record, part 0 writing loss and lse; otherwise from the lse that the caller
 // kept
-template <typename T, bool JOIN, bool GRAD>
+template <typename T, int E, bool JOIN, bool GRAD>
 __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int parts_here) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
   __shared__ float red[48];
@@ -384,10 +386,10 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
   const int part = (int)(blockIdx.x % parts_here), lane = threadIdx.x & 63;
   const Row<T> s(g.logits, row, g.V);
   const int64_t first = part * g.span, last = min(s.vectors(), first + g.span);
-  float x[kPartE][W];
+  float x[E][W];
   if (GRAD) {
 #pragma unroll
-    for (int e = 0; e < kPartE; ++e) {
+    for (int e = 0; e < E; ++e) {
       const int64_t i = first + (int64_t)e * NT + threadIdx.x;
       if (i < last) s.load(i, x[e]);
     }
@@ -435,7 +437,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
   T* o = static_cast<T*>(g.grad) + row * g.V;
   const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
 #pragma unroll
-  for (int e = 0; e < kPartE; ++e) {
+  for (int e = 0; e < E; ++e) {
     const int64_t i = first + (int64_t)e * NT + threadIdx.x;
     if (i < last) {
 #pragma unroll
@@ -450,54 +452,74 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
 }
 
 // ---- which form a call takes ---------------------------------------------------------------------------------------------
-// A part of a row: at most kPartThreads * kPartE vectors.
-struct Split { int parts; int64_t span; };
+// A long row whole: 512 threads of 8 vectors while there are at most two rows a CU, where the time is one workgroup's, 256 of 16
+// beyond, where what counts is how many rows are under way (forward and backward of 10000 float scores, both ways: 64 rows 10.0
+// and 11.9 us, 512 rows 15.9 and 16.9, 1024 rows 27.9 and 21.8).
+// A part of a row is at most kPartThreads * each vectors: one a thread while that makes no more than kFewParts parts, since the
+// code of one is the shortest (8 rows of 131071 bf16 scores, forward and backward: 13.7 us with one, 14.6 with two, 18.5 with
+// eight), more as there are more rows, each part having the row's maximum to find again (100 rows of 131072: 91, 63 and 45 us;
+// with room for 2048 parts 49).
+constexpr int kMostEach = 8, kFewParts = 1024, kFewRows = 512;
+struct Split { int parts, each; int64_t span; };
 int64_t row_vectors(int64_t V, int W) { return (V + W - 1 + W - 1) / W; }  // at the worst offset
 Split split_of(int64_t R, int64_t V, int W) {
-  const int64_t nv = row_vectors(V, W), most = kPartThreads * kPartE;
-  int64_t parts = (nv + most - 1) / most;
-  // few rows: enough parts for 512 workgroups, of at least one vector a thread
-  const int64_t want = (512 + R - 1) / R, fit = (nv + kPartThreads - 1) / kPartThreads;
-  const int64_t more = want < fit ? want : fit;
-  if (parts < more) parts = more;
+  const int64_t nv = row_vectors(V, W);
+  int each = 1;
+  int64_t parts;
+  for (;; each *= 2) {
+    parts = (nv + kPartThreads * each - 1) / (kPartThreads * each);
+    if (each == kMostEach || parts == 1 || R * parts <= kFewParts) break;
+  }
   const int64_t span = (nv + parts - 1) / parts;
-  return Split{(int)((nv + span - 1) / span), span};
+  return Split{(int)((nv + span - 1) / span), each, span};
 }
-bool in_registers(int64_t R, int64_t V, int W) {
-  (void)R;
-  return row_vectors(V, W) <= 256 * 16;
+bool in_registers(int64_t V, int W) { return row_vectors(V, W) <= 256 * 16; }
+
+template <typename F>
+void each(int n, F launch) {
+  if (n == 1) launch(std::integral_constant<int, 1>());
+  else if (n == 2) launch(std::integral_constant<int, 2>());
+  else if (n == 4) launch(std::integral_constant<int, 4>());
+  else launch(std::integral_constant<int, kMostEach>());
 }
 
 template <typename T, bool GRAD>
 void launch_forward(Args a, hipStream_t st) {
   constexpr int W = Row<T>::W;
   const int64_t nv = row_vectors(a.V, W);
-  if (in_registers(a.R, a.V, W)) {
+  if (in_registers(a.V, W)) {
     const dim3 grid((unsigned)a.R);
     if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), 0, st, a);
     else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), 0, st, a);
+    else if (a.R <= kFewRows) hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), 0, st, a);
     else hipLaunchKernelGGL((k_distill_rows<T, 256, 16, GRAD>), grid, dim3(256), 0, st, a);
     return;
   }
   const Split sp = split_of(a.R, a.V, W);
   a.parts = sp.parts;
   a.span = sp.span;
-  hipLaunchKernelGGL((k_distill_stats<T>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), 0, st, a);
   const int here = GRAD ? sp.parts : 1;
-  hipLaunchKernelGGL((k_distill_finish<T, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), 0, st, a, here);
+  each(sp.each, [&](auto e) {
+    constexpr int E = decltype(e)::value;
+    hipLaunchKernelGGL((k_distill_stats<T, E>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), 0, st, a);
+    hipLaunchKernelGGL((k_distill_finish<T, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), 0, st, a, here);
+  });
 }
 template <typename T>
 void launch_backward(Args a, hipStream_t st) {
   const Split sp = split_of(a.R, a.V, Row<T>::W);
   a.parts = sp.parts;
   a.span = sp.span;
-  hipLaunchKernelGGL((k_distill_finish<T, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), 0, st, a, sp.parts);
+  each(sp.each, [&](auto e) {
+    hipLaunchKernelGGL((k_distill_finish<T, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), 0, st,
+                       a, sp.parts);
+  });
 }
 
 size_t need(int64_t R, int64_t V) {
   size_t most = 0;
   for (int W : {4, 8})
-    if (!in_registers(R, V, W)) {
+    if (!in_registers(V, W)) {
       const size_t n = (size_t)R * (sizeof(RowTeacher) + split_of(R, V, W).parts * sizeof(float2));
       if (n > most) most = n;
     }
