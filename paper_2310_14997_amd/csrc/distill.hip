@@ -50,6 +50,7 @@ struct RowTeacher {
 };
 
 // ---- sums and maxima over a workgroup of NT threads, N values at a time, in a fixed order --------------------------------
+// (one barrier: a kernel gives each call 48 floats of its own)
 template <typename F, typename X> __device__ __forceinline__ X across_wave(X v, F f) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
@@ -60,7 +61,6 @@ __device__ __forceinline__ void all(float (&v)[N], float* red, F f) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = across_wave(v[i], f);
   if (NT == 64) return;
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) red[i * 16 + (threadIdx.x >> 6)] = v[i];
@@ -170,13 +170,15 @@ __device__ __forceinline__ Teacher teacher_of(float top, float wrong, float tota
   t.inv = 1.0f / total;
   return t;
 }
-template <typename T, int NT>
-__device__ __forceinline__ Teacher teacher_row(const Args& g, int64_t row, Entries& E, float* red) {
+// between(): what else comes between the barrier that the ids are behind and the last one
+template <typename T, int NT, typename F>
+__device__ __forceinline__ Teacher teacher_row(const Args& g, int64_t row, Entries& E, float* red, F between) {
   float v[2];
   load_entries<T, NT>(g, row, E, &v[0], &v[1]);
   all<NT, 2>(v, red, Max());
+  between();
   float total[1] = {weigh_entries<NT>(g, E, v[0])};
-  all<NT, 1>(total, red, Add());
+  all<NT, 1>(total, red + 48, Add());
   return teacher_of(v[0], v[1], total[0]);
 }
 
@@ -203,53 +205,85 @@ __device__ __forceinline__ float loss_of(const Args& g, bool some, bool bad, dou
   return bad ? NAN : some ? (float)((double)g.tau * g.tau * (terms + sum * lse)) : 0.0f;
 }
 
-// Gradient entries that the teacher has, for ids in [lo, hi): the first of equal ids writes what all of them add up to, in
-// their order.  A thread's first entry is looked at ahead (look: its score is asked for, all ids are looked through for equal
-// ones), while the rest of the row is under way; write comes when the other entries have been written, behind a barrier.
-template <typename T, int NT> struct Writer {
-  const Args& g;
-  const Entries& E;
-  const T* s;
-  int64_t lo, hi;
-  T score;
-  bool first, behind;
-  __device__ __forceinline__ Writer(const Args& g_, const Entries& E_, const T* s_, int64_t lo_, int64_t hi_)
-      : g(g_), E(E_), s(s_), lo(lo_), hi(hi_) {}
-  __device__ __forceinline__ void look(int e) {
-    const int id = e < g.k ? E.id[e] : -1;
-    first = id >= 0 && id >= lo && id < hi;
-    if (!__any(first)) return;
-    if (first) score = s[id];
-    // equal ids: any before this one, any behind it (four at a time; from k on there is no id)
-    bool before = false;
-    behind = false;
-#pragma unroll 4
-    for (int f = 0; f < g.k; f += 4) {
-      const int4 at = *reinterpret_cast<const int4*>(&E.id[f]);
-      const int v[4] = {at.x, at.y, at.z, at.w};
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        before |= v[u] == id && f + u < e;
-        behind |= v[u] == id && f + u > e;
-      }
-    }
-    first = first && !before;
-  }
-  // q_of(score): the softmax's entry; p_of(e): p of entry e
-  template <typename Q, typename P> __device__ __forceinline__ void write(T* o, float scale, Q q_of, P p_of) {
-    for (int e = threadIdx.x; e < g.k; e += NT) {
-      if (e >= NT) look(e);
-      if (!first) continue;
-      const int id = E.id[e];
-      float p = p_of(e);
-      if (behind) {
-        for (int f = e + 1; f < g.k; ++f)
-          if (E.id[f] == id) p += p_of(f);
-      }
-      o[id] = from_float<T>(scale * (q_of(to_float<T>(score)) - p));
-    }
-  }
+// The gradient of a span of the row, E vectors a thread.  The entries that fall into a vector hang from its head as a chain
+// (entry + 1, 0: none), so the thread that has the vector subtracts them before it stores it: no second look at the row, no wait
+// for its stores.  hang comes when the heads are empty and the ids there, each behind a barrier, write behind another.  The
+// chain's order is left open: equal ids are added up in the order of the list.
+template <int N> struct Chains {
+  int head[N];
+  uint16_t next[kMostEntries];
 };
+template <typename T, int NT, int N>
+__device__ __forceinline__ void empty(Chains<N>& c) {
+#pragma unroll
+  for (int e = 0; e < N / NT; ++e) c.head[e * NT + threadIdx.x] = 0;
+}
+template <typename T, int NT, int N>
+__device__ __forceinline__ void hang(const Args& g, const Entries& E, const Row<T>& s, int64_t first, int64_t last, Chains<N>& c) {
+  for (int e = threadIdx.x; e < g.k; e += NT) {
+    const int64_t id = E.id[e], i = (id + s.off) / Row<T>::W;
+    if (id >= 0 && i >= first && i < last) c.next[e] = (uint16_t)atomicExch(&c.head[i - first], e + 1);
+  }
+}
+// x: exp((s - m) / tau), by = scale * inv; p_of(e): p of entry e
+template <typename T, int NT, int E, int N, typename P>
+__device__ __forceinline__ void write(const Args& g, const Entries& ent, const Row<T>& s, int64_t row, int64_t first, int64_t last,
+                                      const Chains<N>& c, const float (&x)[E][Row<T>::W], float scale, float inv, P p_of) {
+  constexpr int W = Row<T>::W;
+  static_assert(N >= NT * E && E <= 32, "a head a vector");
+  T* o = static_cast<T*>(g.grad) + row * g.V;
+  const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
+  const float by = scale * inv;
+  unsigned held = 0;  // vectors with entries: one at a time, by code that is there once
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int64_t i = first + (int64_t)e * NT + threadIdx.x;
+    if (i >= last) continue;
+    if (c.head[e * NT + threadIdx.x] != 0 && scale != 0.0f) {
+      held |= 1u << e;
+      continue;
+    }
+    float v[W];
+#pragma unroll
+    for (int u = 0; u < W; ++u) v[u] = scale == 0.0f ? 0.0f : x[e][u] * by;
+    s.store(o, same, i, v);
+  }
+  while (held) {
+    const int at = __builtin_ctz(held);
+    held &= held - 1;
+    const int64_t i = first + (int64_t)at * NT + threadIdx.x;
+    float q[W], v[W];
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      q[u] = x[0][u];
+#pragma unroll
+      for (int e = 1; e < E; ++e) q[u] = e == at ? x[e][u] : q[u];
+      q[u] *= inv;
+      v[u] = scale * q[u];
+    }
+    unsigned seen = 0, again = 0;
+    const auto put = [&](int w, float p) {
+#pragma unroll
+      for (int u = 0; u < W; ++u) v[u] = u == w ? scale * (q[u] - p) : v[u];
+    };
+    for (int n = c.head[at * NT + threadIdx.x]; n != 0; n = c.next[n - 1]) {
+      const int w = (int)((ent.id[n - 1] + s.off) % W);
+      again |= seen & (1u << w);
+      seen |= 1u << w;
+      put(w, p_of(n - 1));
+    }
+    while (again) {
+      const int w = __builtin_ctz(again);
+      again &= again - 1;
+      const int id = (int)(i * W - s.off + w);
+      float p = 0.0f;
+      for (int e = 0; e < g.k; ++e)
+        if (ent.id[e] == id) p += p_of(e);
+      put(w, p);
+    }
+    s.store(o, same, i, v);
+  }
+}
 
 // what the row's loss counts, and what its gradient is scaled by; 0: the row is all zeros
 __device__ __forceinline__ float row_weight(const Args& g, int64_t row) { return g.grad_loss ? g.grad_loss[row] : 1.0f; }
@@ -262,8 +296,9 @@ __device__ __forceinline__ float row_scale(const Args& g, float weight, bool som
 template <typename T, int NT, int E, bool GRAD>
 __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   constexpr int W = Row<T>::W;
-  __shared__ float red[48];
+  __shared__ float red[96];
   __shared__ Entries ent;
+  __shared__ Chains<GRAD ? NT * E : NT> chains;
   const int64_t row = blockIdx.x;
   const Row<T> s(g.logits, row, g.V);
   const int64_t nv = s.vectors();
@@ -275,6 +310,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   // maxima of the row and of the teacher's scores together, then both sums of exponentials
   float v[3] = {-INFINITY, 0.0f, 0.0f};
   load_entries<T, NT>(g, row, ent, &v[1], &v[2]);
+  if constexpr (GRAD) empty<T, NT>(chains);
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (e * NT < nv) {
@@ -283,8 +319,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
     }
   all<NT, 3>(v, red, Max());  // (behind it every entry's id is in LDS)
   if (NT == 64) __syncthreads();
-  Writer<T, NT> entries(g, ent, s.p, 0, g.V);
-  if (GRAD) entries.look(threadIdx.x);
+  if constexpr (GRAD) hang<T, NT>(g, ent, s, 0, nv, chains);
   const float m = v[0];
   float sums[2] = {0.0f, weigh_entries<NT>(g, ent, v[1])};
 #pragma unroll
@@ -297,24 +332,13 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
         sums[0] += x[e][u];
       }
     }
-  all<NT, 2>(sums, red, Add());
+  all<NT, 2>(sums, red + 48, Add());
+  if (NT == 64) __syncthreads();
   const Teacher tr = teacher_of(v[1], v[2], sums[1]);
   const float inv = 1.0f / sums[0];
-  const float scale = GRAD ? row_scale(g, weight, tr.some, tr.bad) : 0.0f, by = scale * inv;
-  T* o = static_cast<T*>(g.grad) + row * g.V;
-  if (GRAD) {
-    const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (e * NT < nv) {
-#pragma unroll
-        for (int u = 0; u < W; ++u) x[e][u] = scale == 0.0f ? 0.0f : x[e][u] * by;
-        s.store(o, same, (int64_t)e * NT + threadIdx.x, x[e]);
-      }
-  }
-  __syncthreads();
-  if (GRAD && scale != 0.0f) {
-    entries.write(o, scale, [&](float a) { return expf((a - m) * g.inv_tau) * inv; }, [&](int e) { return ent.w[e] * tr.inv; });
+  if constexpr (GRAD) {
+    const float scale = row_scale(g, weight, tr.some, tr.bad);
+    write<T, NT, E>(g, ent, s, row, 0, nv, chains, x, scale, inv, [&](int e) { return ent.w[e] * tr.inv; });
   }
   if (threadIdx.x < 64) {
     double terms, sum;
@@ -334,13 +358,12 @@ constexpr int kPartThreads = 256;
 template <typename T, int E>
 __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
-  __shared__ float red[48];
+  __shared__ float red[96];
   __shared__ Entries ent;
   const int64_t row = blockIdx.x / (g.parts + 1);
   const int part = (int)(blockIdx.x % (g.parts + 1));
   if (part == g.parts) {  // the row's teacher: what the second launch needs of it
-    const Teacher tr = teacher_row<T, NT>(g, row, ent, red);
-    __syncthreads();
+    const Teacher tr = teacher_row<T, NT>(g, row, ent, red, [] {});
     if (threadIdx.x < 64) {
       double terms, all_p;
       loss_terms<T>(g, row, ent, tr, &terms, &all_p);
@@ -371,7 +394,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   for (int e = 0; e < E; ++e)
 #pragma unroll
     for (int u = 0; u < W; ++u) sum[0] += x[e][u] == -INFINITY ? 0.0f : expf((x[e][u] - m) * g.inv_tau);
-  all<NT, 1>(sum, red, Add());
+  all<NT, 1>(sum, red + 48, Add());
   if (threadIdx.x == 0) g.stat[row * g.parts + part] = make_float2(m, sum[0]);
 }
 
@@ -380,14 +403,15 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
 template <typename T, int E, bool JOIN, bool GRAD>
 __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int parts_here) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
-  __shared__ float red[48];
+  __shared__ float red[96];
   __shared__ Entries ent;
+  __shared__ Chains<GRAD ? NT * E : NT> chains;
   const int64_t row = blockIdx.x / parts_here;
   const int part = (int)(blockIdx.x % parts_here), lane = threadIdx.x & 63;
   const Row<T> s(g.logits, row, g.V);
   const int64_t first = part * g.span, last = min(s.vectors(), first + g.span);
   float x[E][W];
-  if (GRAD) {
+  if constexpr (GRAD) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int64_t i = first + (int64_t)e * NT + threadIdx.x;
@@ -395,18 +419,19 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     }
   }
   const float weight = GRAD ? row_weight(g, row) : 0.0f;
-  Writer<T, NT> entries(g, ent, s.p, first * W - s.off, last * W - s.off);
+  if constexpr (GRAD) empty<T, NT>(chains);
   Teacher tr;
   float m, inv;
   if (JOIN) {
     // (every wavefront joins the parts for itself: no barrier to wait at)
     const RowTeacher rec = g.rec[row];
     tr.top = rec.top; tr.inv = rec.inv; tr.some = rec.some; tr.bad = rec.bad;
-    if (GRAD) {
+    if constexpr (GRAD) {
       float a, b;
       load_entries<T, NT>(g, row, ent, &a, &b);
       __syncthreads();
-      entries.look(threadIdx.x);
+      hang<T, NT>(g, ent, s, first, last, chains);
+      __syncthreads();
     }
     m = -INFINITY;
     for (int c = lane; c < g.parts; c += 64) m = fmaxf(m, g.stat[row * g.parts + c].x);
@@ -424,31 +449,18 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
       g.lse[row] = (float)lse;
     }
   } else {
-    tr = teacher_row<T, NT>(g, row, ent, red);
+    tr = teacher_row<T, NT>(g, row, ent, red, [&] { hang<T, NT>(g, ent, s, first, last, chains); });
     m = g.lse_in[row] * g.tau;  // exp((s - tau lse) / tau) is q itself
     inv = 1.0f;
   }
-  if (!GRAD) return;
-  if (!JOIN) {
-    __syncthreads();
-    entries.look(threadIdx.x);
-  }
-  const float scale = row_scale(g, weight, tr.some, tr.bad), by = scale * inv;
-  T* o = static_cast<T*>(g.grad) + row * g.V;
-  const bool same = (((uintptr_t)o ^ (uintptr_t)s.p) & 15) == 0;
+  if constexpr (GRAD) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int64_t i = first + (int64_t)e * NT + threadIdx.x;
-    if (i < last) {
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int u = 0; u < W; ++u) x[e][u] = scale == 0.0f ? 0.0f : expf((x[e][u] - m) * g.inv_tau) * by;
-      s.store(o, same, i, x[e]);
-    }
+      for (int u = 0; u < W; ++u) x[e][u] = expf((x[e][u] - m) * g.inv_tau);
+    write<T, NT, E>(g, ent, s, row, first, last, chains, x, row_scale(g, weight, tr.some, tr.bad), inv,
+                    [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; });
   }
-  if (scale == 0.0f) return;
-  __syncthreads();
-  entries.write(o, scale, [&](float a) { return expf((a - m) * g.inv_tau) * inv; },
-                [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; });
 }
 
 // ---- which form a call takes ---------------------------------------------------------------------------------------------
