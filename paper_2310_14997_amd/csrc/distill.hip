@@ -16,7 +16,7 @@
 namespace spcfg {
 namespace {
 
-constexpr int kMostEntries = 1024;  // of the teacher's, a row: they are kept in LDS
+constexpr int kMostEntries = 1024;  // of the teacher's, a row: they are kept in LDS, 10 bytes each
 
 typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
 
@@ -123,10 +123,14 @@ template <typename T> struct Row {
 };
 
 // ---- the teacher's entries ---------------------------------------------------------------------------------------------
+// in LDS, of k entries: a workgroup of one wavefront takes little of it, so that many fit a CU
 struct Entries {
-  alignas(16) int id[kMostEntries];  // -1 where absent, and up to the next multiple of 4
-  float w[kMostEntries];             // the score, then exp((score - top) / tau)
+  int* id;         // -1 where absent
+  float* w;        // the score, then exp((score - top) / tau)
+  uint16_t* next;  // in a vector's chain
+  __device__ __forceinline__ Entries(int* lds, int k) : id(lds), w(reinterpret_cast<float*>(lds + k)), next(reinterpret_cast<uint16_t*>(lds + 2 * k)) {}
 };
+unsigned entries_bytes(int k) { return (unsigned)(k * 10 + 15) / 16 * 16; }
 struct Teacher {
   float top, inv;       // p = w * inv
   bool some, bad;       // whether any entry is there; whether an id is out of range or a score NaN or +inf
@@ -149,7 +153,6 @@ __device__ __forceinline__ void load_entries(const Args& g, int64_t row, Entries
     E.w[e] = a;
     if (id >= 0) *top = fmaxf(*top, a);
   }
-  if (threadIdx.x < 3 && g.k + threadIdx.x < (unsigned)((g.k + 3) / 4 * 4)) E.id[g.k + threadIdx.x] = -1;
 }
 // E.w from scores to exponentials (each thread its own), and their sum over this thread's
 template <int NT>
@@ -209,26 +212,22 @@ __device__ __forceinline__ float loss_of(const Args& g, bool some, bool bad, dou
 // (entry + 1, 0: none), so the thread that has the vector subtracts them before it stores it: no second look at the row, no wait
 // for its stores.  hang comes when the heads are empty and the ids there, each behind a barrier, write behind another.  The
 // chain's order is left open: equal ids are added up in the order of the list.
-template <int N> struct Chains {
-  int head[N];
-  uint16_t next[kMostEntries];
-};
 template <typename T, int NT, int N>
-__device__ __forceinline__ void empty(Chains<N>& c) {
+__device__ __forceinline__ void empty(int (&head)[N]) {
 #pragma unroll
-  for (int e = 0; e < N / NT; ++e) c.head[e * NT + threadIdx.x] = 0;
+  for (int e = 0; e < N / NT; ++e) head[e * NT + threadIdx.x] = 0;
 }
 template <typename T, int NT, int N>
-__device__ __forceinline__ void hang(const Args& g, const Entries& E, const Row<T>& s, int64_t first, int64_t last, Chains<N>& c) {
+__device__ __forceinline__ void hang(const Args& g, const Entries& E, const Row<T>& s, int64_t first, int64_t last, int (&head)[N]) {
   for (int e = threadIdx.x; e < g.k; e += NT) {
     const int64_t id = E.id[e], i = (id + s.off) / Row<T>::W;
-    if (id >= 0 && i >= first && i < last) c.next[e] = (uint16_t)atomicExch(&c.head[i - first], e + 1);
+    if (id >= 0 && i >= first && i < last) E.next[e] = (uint16_t)atomicExch(&head[i - first], e + 1);
   }
 }
 // x: exp((s - m) / tau), by = scale * inv; p_of(e): p of entry e
 template <typename T, int NT, int E, int N, typename P>
 __device__ __forceinline__ void write(const Args& g, const Entries& ent, const Row<T>& s, int64_t row, int64_t first, int64_t last,
-                                      const Chains<N>& c, const float (&x)[E][Row<T>::W], float scale, float inv, P p_of) {
+                                      const int (&head)[N], const float (&x)[E][Row<T>::W], float scale, float inv, P p_of) {
   constexpr int W = Row<T>::W;
   static_assert(N >= NT * E && E <= 32, "a head a vector");
   T* o = static_cast<T*>(g.grad) + row * g.V;
@@ -239,7 +238,7 @@ __device__ __forceinline__ void write(const Args& g, const Entries& ent, const R
   for (int e = 0; e < E; ++e) {
     const int64_t i = first + (int64_t)e * NT + threadIdx.x;
     if (i >= last) continue;
-    if (c.head[e * NT + threadIdx.x] != 0 && scale != 0.0f) {
+    if (head[e * NT + threadIdx.x] != 0 && scale != 0.0f) {
       held |= 1u << e;
       continue;
     }
@@ -266,7 +265,7 @@ __device__ __forceinline__ void write(const Args& g, const Entries& ent, const R
 #pragma unroll
       for (int u = 0; u < W; ++u) v[u] = u == w ? scale * (q[u] - p) : v[u];
     };
-    for (int n = c.head[at * NT + threadIdx.x]; n != 0; n = c.next[n - 1]) {
+    for (int n = head[at * NT + threadIdx.x]; n != 0; n = ent.next[n - 1]) {
       const int w = (int)((ent.id[n - 1] + s.off) % W);
       again |= seen & (1u << w);
       seen |= 1u << w;
@@ -297,8 +296,9 @@ template <typename T, int NT, int E, bool GRAD>
 __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   constexpr int W = Row<T>::W;
   __shared__ float red[96];
-  __shared__ Entries ent;
-  __shared__ Chains<GRAD ? NT * E : NT> chains;
+  extern __shared__ __attribute__((aligned(16))) int lds[];
+  Entries ent(lds, g.k);
+  __shared__ int head[GRAD ? NT * E : 1];
   const int64_t row = blockIdx.x;
   const Row<T> s(g.logits, row, g.V);
   const int64_t nv = s.vectors();
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   // maxima of the row and of the teacher's scores together, then both sums of exponentials
   float v[3] = {-INFINITY, 0.0f, 0.0f};
   load_entries<T, NT>(g, row, ent, &v[1], &v[2]);
-  if constexpr (GRAD) empty<T, NT>(chains);
+  if constexpr (GRAD) empty<T, NT>(head);
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (e * NT < nv) {
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
     }
   all<NT, 3>(v, red, Max());  // (behind it every entry's id is in LDS)
   if (NT == 64) __syncthreads();
-  if constexpr (GRAD) hang<T, NT>(g, ent, s, 0, nv, chains);
+  if constexpr (GRAD) hang<T, NT>(g, ent, s, 0, nv, head);
   const float m = v[0];
   float sums[2] = {0.0f, weigh_entries<NT>(g, ent, v[1])};
 #pragma unroll
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   const float inv = 1.0f / sums[0];
   if constexpr (GRAD) {
     const float scale = row_scale(g, weight, tr.some, tr.bad);
-    write<T, NT, E>(g, ent, s, row, 0, nv, chains, x, scale, inv, [&](int e) { return ent.w[e] * tr.inv; });
+    write<T, NT, E>(g, ent, s, row, 0, nv, head, x, scale, inv, [&](int e) { return ent.w[e] * tr.inv; });
   }
   if (threadIdx.x < 64) {
     double terms, sum;
@@ -359,7 +359,8 @@ template <typename T, int E>
 __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
   __shared__ float red[96];
-  __shared__ Entries ent;
+  extern __shared__ __attribute__((aligned(16))) int lds[];
+  Entries ent(lds, g.k);
   const int64_t row = blockIdx.x / (g.parts + 1);
   const int part = (int)(blockIdx.x % (g.parts + 1));
   if (part == g.parts) {  // the row's teacher: what the second launch needs of it
@@ -404,8 +405,9 @@ template <typename T, int E, bool JOIN, bool GRAD>
 __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int parts_here) {
   constexpr int W = Row<T>::W, NT = kPartThreads;
   __shared__ float red[96];
-  __shared__ Entries ent;
-  __shared__ Chains<GRAD ? NT * E : NT> chains;
+  extern __shared__ __attribute__((aligned(16))) int lds[];
+  Entries ent(lds, g.k);
+  __shared__ int head[GRAD ? NT * E : 1];
   const int64_t row = blockIdx.x / parts_here;
   const int part = (int)(blockIdx.x % parts_here), lane = threadIdx.x & 63;
   const Row<T> s(g.logits, row, g.V);
@@ -419,7 +421,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     }
   }
   const float weight = GRAD ? row_weight(g, row) : 0.0f;
-  if constexpr (GRAD) empty<T, NT>(chains);
+  if constexpr (GRAD) empty<T, NT>(head);
   Teacher tr;
   float m, inv;
   if (JOIN) {
@@ -430,7 +432,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
       float a, b;
       load_entries<T, NT>(g, row, ent, &a, &b);
       __syncthreads();
-      hang<T, NT>(g, ent, s, first, last, chains);
+      hang<T, NT>(g, ent, s, first, last, head);
       __syncthreads();
     }
     m = -INFINITY;
@@ -449,7 +451,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
       g.lse[row] = (float)lse;
     }
   } else {
-    tr = teacher_row<T, NT>(g, row, ent, red, [&] { hang<T, NT>(g, ent, s, first, last, chains); });
+    tr = teacher_row<T, NT>(g, row, ent, red, [&] { hang<T, NT>(g, ent, s, first, last, head); });
     m = g.lse_in[row] * g.tau;  // exp((s - tau lse) / tau) is q itself
     inv = 1.0f;
   }
@@ -458,7 +460,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int u = 0; u < W; ++u) x[e][u] = expf((x[e][u] - m) * g.inv_tau);
-    write<T, NT, E>(g, ent, s, row, first, last, chains, x, row_scale(g, weight, tr.some, tr.bad), inv,
+    write<T, NT, E>(g, ent, s, row, first, last, head, x, row_scale(g, weight, tr.some, tr.bad), inv,
                     [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; });
   }
 }
@@ -499,12 +501,13 @@ template <typename T, bool GRAD>
 void launch_forward(Args a, hipStream_t st) {
   constexpr int W = Row<T>::W;
   const int64_t nv = row_vectors(a.V, W);
+  const unsigned lds = entries_bytes(a.k);
   if (in_registers(a.V, W)) {
     const dim3 grid((unsigned)a.R);
-    if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), 0, st, a);
-    else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), 0, st, a);
-    else if (a.R <= kFewRows) hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_distill_rows<T, 256, 16, GRAD>), grid, dim3(256), 0, st, a);
+    if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), lds, st, a);
+    else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), lds, st, a);
+    else if (a.R <= kFewRows) hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), lds, st, a);
+    else hipLaunchKernelGGL((k_distill_rows<T, 256, 16, GRAD>), grid, dim3(256), lds, st, a);
     return;
   }
   const Split sp = split_of(a.R, a.V, W);
@@ -513,8 +516,8 @@ void launch_forward(Args a, hipStream_t st) {
   const int here = GRAD ? sp.parts : 1;
   each(sp.each, [&](auto e) {
     constexpr int E = decltype(e)::value;
-    hipLaunchKernelGGL((k_distill_stats<T, E>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), 0, st, a);
-    hipLaunchKernelGGL((k_distill_finish<T, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), 0, st, a, here);
+    hipLaunchKernelGGL((k_distill_stats<T, E>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), lds, st, a);
+    hipLaunchKernelGGL((k_distill_finish<T, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), lds, st, a, here);
   });
 }
 template <typename T>
@@ -522,8 +525,9 @@ void launch_backward(Args a, hipStream_t st) {
   const Split sp = split_of(a.R, a.V, Row<T>::W);
   a.parts = sp.parts;
   a.span = sp.span;
+  const unsigned lds = entries_bytes(a.k);
   each(sp.each, [&](auto e) {
-    hipLaunchKernelGGL((k_distill_finish<T, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), 0, st,
+    hipLaunchKernelGGL((k_distill_finish<T, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), lds, st,
                        a, sp.parts);
   });
 }
