@@ -216,3 +216,38 @@ def test_tables_of_more_than_32_bits_of_bytes():
         bd.spcfg_distill_backward(s, t, ids, 1.0, e, None, gr)
         close("gradient from lse", values(gr[pick]), grad, (2.0 ** -8 + 2.0 ** -16) * np.abs(grad) + 2.0 ** -16 * np.exp(values(s[pick]) - lse[:, None]) + 2.0 ** -20 * (grad < 0))
         del s, gr
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("R,V,k", [(20, 70001, 16), (50, 70001, 16), (70, 70001, 16), (520, 4203, 5), (520, 9001, 5), (700, 250, 9)])
+def test_many_rows(R, V, k, bf16):
+    """Parts of two, four and eight vectors a thread, rows whole in 256 threads, short rows of a wavefront each."""
+    print("case distill rows", R, V, k, bf16, flush=True)
+    check(inputs(R, V, k, bf16), 1.5, bf16)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [300, 5000, 40003])
+def test_entries_side_by_side(V, bf16):
+    """Every element of a stretch with an entry, some with two or more, and a row whose entries all have one id: twice the same."""
+    import torch
+    R, k = 5, 256
+    s, t, ids, g = inputs(R, V, k, bf16, seed=4)
+    order = np.random.default_rng(6).permutation(k)
+    ids[0] = order
+    ids[1] = V - 1 - order // 2
+    ids[2] = 17
+    ids[3] = np.where(order < 250, order % 5, -1)
+    ids[4] = V - 1
+    g[:] = 1.25
+    # p of equal ids is added up in 64 bits and rounded once more: 2^-24 within the 2^-20 that an entry is allowed
+    check((s, t, ids, g), 2.0, bf16, 1)
+    ts, tt, ti = put(s, dtype(bf16)), put(t, dtype(bf16)), put(ids, torch.int32)
+    l, e, ws = torch.empty(R, device="cuda:0"), torch.empty(R, device="cuda:0"), scratch(R, V)
+    a, b = (torch.empty(R, V, dtype=dtype(bf16), device="cuda:0") for _ in range(2))
+    for out in (a, b):
+        bd.spcfg_distill_forward_backward(ts, tt, ti, 2.0, None, l, e, out, ws)
+    assert torch.equal(a, b)
+    for out in (a, b):
+        bd.spcfg_distill_backward(ts, tt, ti, 2.0, e, None, out)
+    assert torch.equal(a, b)
