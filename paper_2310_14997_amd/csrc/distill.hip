@@ -33,7 +33,7 @@ struct Args {
   int64_t R, V;
   int k, parts;         // parts of a row along V, `span` vectors of 16 bytes each
   int64_t span;
-  float tau, inv_tau;
+  float tau, by_two;    // by_two: log2(e) / tau
   const void *logits, *teacher;
   const int32_t* ids;
   const float* grad_loss;
@@ -48,6 +48,10 @@ struct RowTeacher {
   int some, bad;
   double terms, sum;    // sum of p (log p - s / tau), sum of p
 };
+
+// exp(d / tau), d <= 0: three roundings of the exponent, as many as exp of d * (1 / tau) has, and a unit of the power; below 2^-126
+// 0.  (With expf, which splits its argument, 4096 rows of 8000 bf16 scores take 38.8 us instead of 34.0.)
+__device__ __forceinline__ float power(const Args& g, float d) { return __builtin_amdgcn_exp2f(d * g.by_two); }
 
 // ---- sums and maxima over a workgroup of NT threads, N values at a time, in a fixed order --------------------------------
 // (one barrier: a kernel gives each call 48 floats of its own)
@@ -159,7 +163,7 @@ template <int NT>
 __device__ __forceinline__ float weigh_entries(const Args& g, Entries& E, float top) {
   float total = 0.0f;
   for (int e = threadIdx.x; e < g.k; e += NT) {
-    const float w = E.id[e] >= 0 ? expf((E.w[e] - top) * g.inv_tau) : 0.0f;
+    const float w = E.id[e] >= 0 ? power(g, E.w[e] - top) : 0.0f;
     E.w[e] = w;
     total += w;
   }
@@ -328,7 +332,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         // outside the row -inf gives 0, unless the whole row is -inf: NaN, as the definition has it
-        x[e][u] = expf((x[e][u] - m) * g.inv_tau);
+        x[e][u] = power(g, x[e][u] - m);
         sums[0] += x[e][u];
       }
     }
@@ -394,7 +398,7 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
 #pragma unroll
   for (int e = 0; e < E; ++e)
 #pragma unroll
-    for (int u = 0; u < W; ++u) sum[0] += x[e][u] == -INFINITY ? 0.0f : expf((x[e][u] - m) * g.inv_tau);
+    for (int u = 0; u < W; ++u) sum[0] += x[e][u] == -INFINITY ? 0.0f : power(g, x[e][u] - m);
   all<NT, 1>(sum, red + 48, Add());
   if (threadIdx.x == 0) g.stat[row * g.parts + part] = make_float2(m, sum[0]);
 }
@@ -441,7 +445,7 @@ __global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
     float sum = 0.0f;
     for (int c = lane; c < g.parts; c += 64) {
       const float2 v = g.stat[row * g.parts + c];
-      sum += v.y * expf((v.x - m) * g.inv_tau);  // a part of nothing but -inf adds 0, a row of nothing else gives NaN
+      sum += v.y * power(g, v.x - m);  // a part of nothing but -inf adds 0, a row of nothing else gives NaN
     }
     sum = across_wave(sum, Add());
     inv = 1.0f / sum;
@@ -463,16 +467,17 @@ __global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int u = 0; u < W; ++u) x[e][u] = expf((x[e][u] - m) * g.inv_tau);
+      for (int u = 0; u < W; ++u) x[e][u] = power(g, x[e][u] - m);
     write<T, NT, E>(g, ent, s, row, first, last, head, x, row_scale(g, weight, tr.some, tr.bad), inv,
-                    [&](int e) { return (JOIN ? expf((ent.w[e] - tr.top) * g.inv_tau) : ent.w[e]) * tr.inv; });
+                    [&](int e) { return (JOIN ? power(g, ent.w[e] - tr.top) : ent.w[e]) * tr.inv; });
   }
 }
 
 // ---- which form a call takes ---------------------------------------------------------------------------------------------
-// A long row whole: 512 threads of 8 vectors while there are at most two rows a CU, where the time is one workgroup's, 256 of 16
-// beyond, where what counts is how many rows are under way (forward and backward of 10000 float scores, both ways: 64 rows 10.0
-// and 11.9 us, 512 rows 15.9 and 16.9, 1024 rows 27.9 and 21.8).
+// A long row whole: 512 threads, so that a row is on its way at once and the registers allow two or more rows a CU, or 256 where
+// that leaves fewer threads idle (forward and backward, threads x vectors: 2048 rows of 10000 bf16 scores, 1251 vectors: 256 x 6
+// 28.6 us, 512 x 3 31.6, 256 x 16 46.6, but 64 rows 9.8 and 8.0; 64 rows of 10000 floats, 2500 vectors: 512 x 5 8.0, 256 x 10 10.7,
+// 2048 rows 34.2 and 33.4; 4096 rows of 30000 bf16 scores: 512 x 8 145, 256 x 16 205).
 // A part of a row is at most kPartThreads * each vectors: one a thread while that makes no more than kFewParts parts, since the
 // code of one is the shortest (8 rows of 131071 bf16 scores, forward and backward: 13.7 us with one, 14.6 with two, 18.5 with
 // eight), more as there are more rows, each part having the row's maximum to find again (100 rows of 131072: 91, 63 and 45 us;
@@ -511,8 +516,10 @@ void launch_forward(Args a, hipStream_t st) {
     if (nv <= 64 * 2) hipLaunchKernelGGL((k_distill_rows<T, 64, 2, GRAD>), grid, dim3(64), lds, st, a);
     else if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), lds, st, a);
     else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), lds, st, a);
-    else if (a.R <= kFewRows) hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), lds, st, a);
-    else hipLaunchKernelGGL((k_distill_rows<T, 256, 16, GRAD>), grid, dim3(256), lds, st, a);
+    else if (a.R <= kFewRows && nv <= 512 * 3) hipLaunchKernelGGL((k_distill_rows<T, 512, 3, GRAD>), grid, dim3(512), lds, st, a);
+    else if (nv <= 256 * 6) hipLaunchKernelGGL((k_distill_rows<T, 256, 6, GRAD>), grid, dim3(256), lds, st, a);
+    else if (nv <= 512 * 5) hipLaunchKernelGGL((k_distill_rows<T, 512, 5, GRAD>), grid, dim3(512), lds, st, a);
+    else hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), lds, st, a);
     return;
   }
   const Split sp = split_of(a.R, a.V, W);
@@ -571,12 +578,13 @@ int check(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, 
   const int rc = check_sizes(rows, V);
   if (rc) return rc;
   if (k < 1 || k > kMostEntries) return SPCFG_ERR_SHAPE;
-  if (!(tau > 0.0f) || !(tau < INFINITY) || !(1.0f / tau < INFINITY)) return SPCFG_ERR_ARG;
+  const double by_two = 1.4426950408889634 / tau;
+  if (!(tau > 0.0f) || !(tau < INFINITY) || !((float)by_two < INFINITY)) return SPCFG_ERR_ARG;
   if (rows > 0 && (!logits || !teacher || !ids)) return SPCFG_ERR_ARG;
   const uintptr_t mask = type == SPCFG_TYPE_F32 ? 3 : 1;
   if (((uintptr_t)logits & mask) || ((uintptr_t)teacher & mask) || ((uintptr_t)ids & 3)) return SPCFG_ERR_ARG;
   *a = Args{};
-  a->R = rows; a->V = V; a->k = k; a->tau = tau; a->inv_tau = 1.0f / tau;
+  a->R = rows; a->V = V; a->k = k; a->tau = tau; a->by_two = (float)by_two;
   a->logits = logits; a->teacher = teacher; a->ids = ids;
   return SPCFG_OK;
 }

@@ -1,7 +1,7 @@
 """GPU tests of distillation from a teacher's top entries against the 64-bit oracle.
 
-Tolerances from the roundings on the way, with u = 2^-24: the sum of exponentials is good to 2^-19 (its argument 2 u |x| e^x
-per term, expf 2 u, at most 100 additions on the way to the result), so lse is good to 2^-19 + u |lse|; p to 2^-20; the loss's
+Tolerances from the roundings on the way, with u = 2^-24: the sum of exponentials is good to 2^-19 (its argument 3 u |x| e^x
+per term, its power 2 u, at most 100 additions on the way to the result), so lse is good to 2^-19 + u |lse|; p to 2^-20; the loss's
 terms are summed in 64 bits: tau^2 (2^-19 + 2^-20 sum p (|log p| + |log q|)) + u |loss|; a gradient to
 |g| tau (2^-18 q + 2^-20 p) plus half a step of its type (2^-24, bf16 2^-8).  From a kept lse, rounded to 32 bits, q is off by
 another 2^-23 (|lse| + |s| / tau).  Numbers below the smallest normal one of 32 bits, 2^-126, may come out as 0: a softmax's entry
