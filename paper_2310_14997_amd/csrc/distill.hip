@@ -3,11 +3,11 @@
 //   p = softmax(t / tau) over the entries that are there,   q = softmax(s / tau) over the row,   lse = log sum exp(s / tau)
 //   loss = tau^2 sum_e p_e (log p_e - log q_id(e)),         d loss / d s_j = tau (q_j - sum_{e: id(e) = j} p_e)
 // Bound by HBM: the row is read once and its gradient written once.  A row that a workgroup can hold in registers is one
-// pass; longer rows, and few rows, are split over workgroups along V: one launch leaves each part's maximum and sum of
-// exponentials (and, once a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p
-// are in 32 bits; logarithms and the sum over the teacher's entries, whose terms cancel where q is near p, in 64.
-// 2048 rows of 10000 floats, k = 64: 37 us (4.4 TB/s; a copy of that size 30).  8 rows of 131071 bf16, k = 128: 14 us, two
-// latencies.
+// pass; longer rows are split over workgroups along V: one launch leaves each part's maximum and sum of exponentials (and, once
+// a row, the teacher's part), a second one joins them and writes the gradient.  Maxima, sums and p are in 32 bits; logarithms
+// and the sum over the teacher's entries, whose terms cancel where q is near p, in 64, and so is the sum of p of equal ids.
+// 2048 rows of 10000 floats, k = 64, forward and backward: 32.6 us (5.0 TB/s; a copy of that size 30).  8 rows of 131071 bf16,
+// k = 128: 9.3 us, two launches one behind the other.
 #include <cmath>
 #include <type_traits>
 
@@ -132,7 +132,8 @@ struct Entries {
   int* id;         // -1 where absent
   float* w;        // the score, then exp((score - top) / tau)
   uint16_t* next;  // in a vector's chain
-  __device__ __forceinline__ Entries(int* lds, int k) : id(lds), w(reinterpret_cast<float*>(lds + k)), next(reinterpret_cast<uint16_t*>(lds + 2 * k)) {}
+  __device__ __forceinline__ Entries(int* lds, int k)
+      : id(lds), w(reinterpret_cast<float*>(lds + k)), next(reinterpret_cast<uint16_t*>(lds + 2 * k)) {}
 };
 unsigned entries_bytes(int k) { return (unsigned)(k * 10 + 15) / 16 * 16; }
 struct Teacher {
@@ -222,7 +223,8 @@ __device__ __forceinline__ void empty(int (&head)[N]) {
   for (int e = 0; e < N / NT; ++e) head[e * NT + threadIdx.x] = 0;
 }
 template <typename T, int NT, int N>
-__device__ __forceinline__ void hang(const Args& g, const Entries& E, const Row<T>& s, int64_t first, int64_t last, int (&head)[N]) {
+__device__ __forceinline__ void hang(const Args& g, const Entries& E, const Row<T>& s, int64_t first, int64_t last,
+                                     int (&head)[N]) {
   for (int e = threadIdx.x; e < g.k; e += NT) {
     const int64_t id = E.id[e], i = (id + s.off) / Row<T>::W;
     if (id >= 0 && i >= first && i < last) E.next[e] = (uint16_t)atomicExch(&head[i - first], e + 1);
@@ -478,10 +480,10 @@ __global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
 // that leaves fewer threads idle (forward and backward, threads x vectors: 2048 rows of 10000 bf16 scores, 1251 vectors: 256 x 6
 // 28.6 us, 512 x 3 31.6, 256 x 16 46.6, but 64 rows 9.8 and 8.0; 64 rows of 10000 floats, 2500 vectors: 512 x 5 8.0, 256 x 10 10.7,
 // 2048 rows 34.2 and 33.4; 4096 rows of 30000 bf16 scores: 512 x 8 145, 256 x 16 205).
-// A part of a row is at most kPartThreads * each vectors: one a thread while that makes no more than kFewParts parts, since the
-// code of one is the shortest (8 rows of 131071 bf16 scores, forward and backward: 13.7 us with one, 14.6 with two, 18.5 with
-// eight), more as there are more rows, each part having the row's maximum to find again (100 rows of 131072: 91, 63 and 45 us;
-// with room for 2048 parts 49).
+// A part of a row is at most kPartThreads * each vectors: one a thread while that makes no more than kFewParts parts, the shortest
+// way from the scores to the gradient (8 rows of 131071 bf16 scores, forward and backward: 9.3 us, with eight a thread 14.1), more as
+// there are more rows, since each part reads the teacher's entries and the row's other parts' sums (100 rows of 131072 25.8 us, with
+// one a thread 31.4).
 constexpr int kMostEach = 8, kFewParts = 1024, kFewRows = 512;
 struct Split { int parts, each; int64_t span; };
 int64_t row_vectors(int64_t V, int W) { return (V + W - 1 + W - 1) / W; }  // at the worst offset
@@ -529,14 +531,15 @@ void launch_forward(Args a, hipStream_t st) {
   each(sp.each, [&](auto e) {
     constexpr int E = decltype(e)::value;
     hipLaunchKernelGGL((k_distill_stats<T, E>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), lds, st, a);
-    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), lds, st, a, here);
+    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)),
+                       dim3(kPartThreads), lds, st, a, here);
   });
 }
 template <typename T>
 void launch_backward(Args a, hipStream_t st) {
   const int64_t nv = row_vectors(a.V, Row<T>::W);
   const unsigned lds = entries_bytes(a.k);
-  // many short rows: 8192 rows of 300 floats 11.1 us, 16.2 with 256 threads a row; 60 rows 4.7 and 4.4
+  // many short rows: 8192 rows of 300 floats 11.1 us, 16.2 with 256 threads a row; 60 rows 4.7 and 4.4 us
   if (nv <= 64 * 2 && a.R > kFewRows) {
     a.parts = 1;
     a.span = nv;
@@ -547,8 +550,8 @@ void launch_backward(Args a, hipStream_t st) {
   a.parts = sp.parts;
   a.span = sp.span;
   each(sp.each, [&](auto e) {
-    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads), lds, st,
-                       a, sp.parts);
+    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)),
+                       dim3(kPartThreads), lds, st, a, sp.parts);
   });
 }
 
