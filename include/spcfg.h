@@ -292,7 +292,7 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
  *   logits         dev [rows x V]            the student's scores, of `type` (SPCFG_TYPE_*)
  *   teacher_logits dev [rows x k], teacher_ids dev [rows x k] int32: the teacher's kept entries of each row, in any order;
  *                  an entry with a negative id, or a score of -inf, is absent.  Equal ids add up.  1 <= k <= 1024
- *   temperature    > 0, finite
+ *   temperature    > 0, finite, and so is 1.5 / temperature
  *   loss, lse      dev [rows] float: out
  *   grad_loss      dev [rows] float or NULL (= all ones): what each row's loss counts in the sum that is differentiated
  *   grad_logits    dev [rows x V] of `type`: grad_loss * temperature * (q_j - sum of the p_e with id(e) = j); overwritten,

@@ -287,10 +287,12 @@ def _here(t, name, shape, dtype, dev):
     """Pointer of a contiguous tensor of that element type and shape on device `dev`; None stays None."""
     if t is None:
         return None
-    if not (isinstance(t, _torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape
-            and t.is_contiguous()):
-        _refuse(t, name, shape, dtype, dev)
-    return t.data_ptr()
+    try:  # (only a tensor has one of torch's dtypes)
+        if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, shape, dtype, dev)
 
 
 def _scratch(t, dev):
