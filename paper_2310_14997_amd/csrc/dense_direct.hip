@@ -72,9 +72,11 @@ __device__ __forceinline__ void product(const Pieces<uint16_t>& a, const Pieces<
 }
 
 // v[i] = element (row, k + i), i = 0 .. 7, of an operand that runs along k; zero from K on (what is loaded there is the row's last,
-// so that no load hangs on a branch).  VEC: base and rows lie on 16 bytes and K is a multiple of 8.
+// so that no load hangs on a branch).  VEC: base and rows lie on 16 bytes and K is a multiple of 8; otherwise whole chunks are
+// read 16 bytes at a time as well, wherever they lie, and only a row's last chunk value by value (fp32 333 x 141 x 474 forward and
+// backward 4.6 and 9.1 us, value by value throughout 6.2 and 11.7).
 template <typename T, bool VEC>
-__device__ __forceinline__ void along(const T* __restrict__ row, int64_t k, int64_t K, T (&v)[8]) {
+__device__ __forceinline__ void along(const T* __restrict__ row, int64_t k, int64_t K, bool whole, T (&v)[8]) {
   if (VEC) {
     const uintx4* p = reinterpret_cast<const uintx4*>(row + min(k, K - 8));
     uintx4 w[sizeof(T) / 2];
@@ -83,6 +85,8 @@ __device__ __forceinline__ void along(const T* __restrict__ row, int64_t k, int6
     __builtin_memcpy(v, w, sizeof(v));
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = k < K ? v[i] : T(0);
+  } else if (whole) {
+    __builtin_memcpy(v, row + k, sizeof(v));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = row[min(k + i, K - 1)];
@@ -134,13 +138,14 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
     for (int u = 0; u < U; ++u) {
       if (u > 0 && c0 + kWaves * u >= chunks) break;
       const int64_t k = (c0 + kWaves * u) * KC + fh * 8;
+      const bool whole = (c0 + kWaves * u + 1) * KC <= K;
       if constexpr (FORM == FWD) {
-        along<TI, VEC>(x + ra * g.I, k, K, va[u]);
-        along<TI, VEC>(W + rb * g.I, k, K, vb[u]);
+        along<TI, VEC>(x + ra * g.I, k, K, whole, va[u]);
+        along<TI, VEC>(W + rb * g.I, k, K, whole, vb[u]);
       } else {
         if constexpr (FORM == DX) {
-          along<TO, VEC>(gy + ra * g.O, k, K, va[u]);
-          if (slope) along<TO, VEC>(z + ra * g.O, k, K, vz[u]);
+          along<TO, VEC>(gy + ra * g.O, k, K, whole, va[u]);
+          if (slope) along<TO, VEC>(z + ra * g.O, k, K, whole, vz[u]);
         } else {
           across<TO>(gy, g.O, ra, k, K, va[u]);
           if (slope) across<TO>(z, g.O, ra, k, K, vz[u]);
@@ -181,7 +186,7 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
   float* bl = lds + kWaves * T * T;  // [wave][64]
   if (FORM == DW) bl[wave * 64 + lane] = bsum;
   __syncthreads();
-  const Epilogue<TI, TO, FORM> ep(g, N);
+  const Epilogue<TI, TO, FORM> ep(g);
   for (int e = threadIdx.x; e < T * T; e += 64 * kWaves) {
     const int64_t m = m0 + e / T, n = n0 + e % T;
     if (m >= rows || n >= N) continue;
@@ -221,7 +226,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_dense_backward(Args g, unsigned
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
 
 // Tiles of 16 where there are few of 32, or no more than 16 rows (us on 16 / 32: fp32 30 x 512 x 512 4.8 / 7.7,
-// 333 x 141 x 474 7.9 / 6.2, backward 11.6 / 15.4, 200 x 512 x 512 backward 15.7 / 11, 1 x 512 x 10000 8.9 / 10.5).
+// 333 x 141 x 474 5.7 / 4.6, backward 8.7 / 9.9, 200 x 512 x 512 backward 15.7 / 11, 1 x 512 x 10000 8.9 / 10.5).
 constexpr int kFew = 160;
 
 template <typename TI, typename TO, int T>
@@ -254,7 +259,7 @@ void backward(const Args& a, hipStream_t st) {
 
 // 3 us to start and end; then whichever is longer, the trips of one wavefront through k (counted in 128 values of a workgroup) or
 // those of all tiles on the whole chip, both fitted.  Measured (us for this kernel / on tiles in LDS): forward fp32 512^3 8.3 / 14,
-// 2048 x 512 x 512 22 / 18, 300 x 2000 x 300 16 / 24, 1000 x 700 x 900 65 / 23, bf16 5.5 / 6.9, 12 / 7.2, 9.0 / 18, 62 / 16;
+// 2048 x 512 x 512 22 / 18, 300 x 2000 x 300 16 / 24, 1000 x 701 x 900 25 / 22, bf16 5.5 / 6.9, 12 / 7.2, 9.0 / 18, 28 / 14;
 // backward fp32 512^3 20 / 19, 2000 x 30 x 30 15 / 22, 300 x 2000 x 300 40 / 25, bf16 12.2 / 11.6, 13 / 21, 26 / 13.
 double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int what) {
   const bool fp32 = in_type == SPCFG_TYPE_F32;
@@ -264,7 +269,7 @@ double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int what) {
   if (what == FORWARD) {
     count = n(R, O);
     longest = (fp32 ? 0.4 : 0.2) * trips(I);
-    all = (I % 8 ? 0.007 : fp32 ? 0.0045 : 0.0021) * count * trips(I);
+    all = (fp32 ? 0.0045 : I % 8 ? 0.0042 : 0.0021) * count * trips(I);
   }
   if (what & BACK_X) {
     count += n(R, I);

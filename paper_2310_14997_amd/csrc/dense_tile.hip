@@ -84,9 +84,9 @@ template <int PL_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct 
 
 #define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
 
-// eight floats of a row of which `left` are there; vec: rows lie on 16 bytes
-__device__ __forceinline__ void put_floats(float* p, const float (&s)[8], int64_t left, bool vec) {
-  if (vec && left >= 8) {
+// eight floats of a row of which `left` are there
+__device__ __forceinline__ void put_floats(float* p, const float (&s)[8], int64_t left) {
+  if (left >= 8) {
     put<float, 4>(p, {s[0], s[1], s[2], s[3]});
     put<float, 4>(p + 4, {s[4], s[5], s[6], s[7]});
   } else {
@@ -95,8 +95,8 @@ __device__ __forceinline__ void put_floats(float* p, const float (&s)[8], int64_
       if (u < left) p[u] = s[u];
   }
 }
-__device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_t left, bool vec) {
-  if (vec && left >= 8) {
+__device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_t left) {
+  if (left >= 8) {
     float a[4], b[4];
     get<float, 4>(p, a);
     get<float, 4>(p + 4, b);
@@ -372,7 +372,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
   float* out = reinterpret_cast<float*>(lds) + wave * 32 * LR;
   const int odd = lane / PER_ROW % 2 * 4;
   const int64_t mw = m0 + wm * MI * 32 + lane / PER_ROW, c = n0 + wn * NI * 32 + lane % PER_ROW * 8;
-  const Epilogue<TI, TO, FORM> ep(g, p.N);
+  const Epilogue<TI, TO, FORM> ep(g);
   float* part = p.splits > 1 ? p.partial + (int64_t)split * p.M * p.N : nullptr;
   float bias[8];
 #pragma unroll
@@ -408,7 +408,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 #pragma unroll
         for (int u = 0; u < 8; ++u) s[u] = __builtin_amdgcn_ldexpf(s[u], -(e + down[u]));
       }
-      if (part) put_floats(part + m * p.N + c, s, p.N - c, (p.N & 3) == 0);
+      if (part) put_floats(part + m * p.N + c, s, p.N - c);
       else ep.eight(m * p.N + c, s, bias, p.N - c);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -464,13 +464,12 @@ __global__ void __launch_bounds__(64 * S::NW, waves_per_simd<S>())
 template <typename TI, typename TO, int FORM>
 __device__ __forceinline__ void join(const Args& g, const Product& p, unsigned block, unsigned blocks) {
   const int64_t per_row = (p.N + 7) / 8, n = p.M * per_row, all = p.M * p.N;
-  const Epilogue<TI, TO, FORM> ep(g, p.N);
-  const bool vec = (p.N & 3) == 0;
+  const Epilogue<TI, TO, FORM> ep(g);
   for (int64_t e = (int64_t)block * 256 + threadIdx.x; e < n; e += (int64_t)blocks * 256) {
     const int64_t m = e / per_row, c = (e - m * per_row) * 8;
     float s[8] = {}, bias[8];
 #pragma unroll 4
-    for (int q = 0; q < p.splits; ++q) add_floats(p.partial + q * all + m * p.N + c, s, p.N - c, vec);
+    for (int q = 0; q < p.splits; ++q) add_floats(p.partial + q * all + m * p.N + c, s, p.N - c);
 #pragma unroll
     for (int u = 0; u < 8; ++u) bias[u] = ep.bias_of(c + u, p.N);
     ep.eight(m * p.N + c, s, bias, p.N - c);
@@ -506,17 +505,20 @@ __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t, const float (
 }
 
 // eight values of a row from column c on, zero outside the matrix (where the nearest ones inside are loaded: no load hangs on a
-// branch of its own)
+// branch of its own).  The eight that hold a row's end are its last, moved down.
 template <typename T>
-__device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, bool vec,
-                                      float (&v)[8]) {
+__device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, int64_t cols, int64_t r, int64_t c, float (&v)[8]) {
   T x[8];
   const T* row = src + min(r, rows - 1) * cols;
-  if (vec) {  // (cols is a multiple of 8)
-    uintx4 w[sizeof(T) / 2];
+  if (cols >= 8) {
+    __builtin_memcpy(x, row + min(c, cols - 8), sizeof(x));
+    if (cols & 7) {
+      const int by = (int)min(c - min(c, cols - 8), (int64_t)7);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uintx4*>(row + min(c, cols - 8))[i];
-    __builtin_memcpy(x, w, sizeof(x));
+      for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8 - d; ++i) x[i] = by & d ? x[i + d] : x[i];
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = row[min(c + i, cols - 1)];
@@ -538,9 +540,8 @@ __device__ __forceinline__ void cut(const T* __restrict__ src, uint16_t* __restr
     r = e / ld;
     c = e - r * ld;
   }
-  const bool vec = ((uintptr_t)src & 15) == 0 && (cols & 7) == 0;
   float v[8];
-  eight<T>(src, rows, cols, r, c, vec, v);
+  eight<T>(src, rows, cols, r, c, v);
   put_planes(dst + e, rows32 * ld, v, T());
 }
 
@@ -556,17 +557,16 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
   const int64_t r1 = min(rows32, (int64_t)(part + 1) * span);
   const TO* gy = static_cast<const TO*>(g.grad_y);
   const TO* z = static_cast<const TO*>(g.preact_in);
-  const bool vec = (((uintptr_t)gy | (uintptr_t)z) & 15) == 0 && (g.O & 7) == 0;
   float s[8] = {};
   if (c < ld) {
     // (four rows' loads in flight)
     for (int64_t r0 = (int64_t)part * span + wave; r0 < r1; r0 += 16) {
       float d[4][8], y[4][8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) eight<TO>(gy, g.R, g.O, r0 + 4 * u, c, vec, d[u]);
+      for (int u = 0; u < 4; ++u) eight<TO>(gy, g.R, g.O, r0 + 4 * u, c, d[u]);
       if (g.act != SPCFG_ACT_NONE) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) eight<TO>(z, g.R, g.O, r0 + 4 * u, c, vec, y[u]);
+        for (int u = 0; u < 4; ++u) eight<TO>(z, g.R, g.O, r0 + 4 * u, c, y[u]);
 #pragma unroll
         for (int u = 0; u < 4; ++u) times_slopes<8>(g.act, y[u], d[u]);
       }
@@ -627,21 +627,20 @@ __global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
   if (r >= h.rows[w]) return;  // (whole groups at a time)
   const float* src = h.src[w];
   const int64_t cols = h.cols, ld = (cols + 31) / 32 * 32;
-  const bool vec = ((uintptr_t)src & 15) == 0 && (cols & 7) == 0;
   constexpr int E = 4;
   float v[E][8];
   float m = 0.0f;
   const bool kept = ld <= (int64_t)G * 8 * E;
   if (kept) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) eight<float>(src, h.rows[w], cols, r, ((int64_t)e * G + gl) * 8, vec, v[e]);
+    for (int e = 0; e < E; ++e) eight<float>(src, h.rows[w], cols, r, ((int64_t)e * G + gl) * 8, v[e]);
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[e][i]));
   } else {
     for (int64_t c = gl * 8; c < ld; c += G * 8) {
-      eight<float>(src, h.rows[w], cols, r, c, vec, v[0]);
+      eight<float>(src, h.rows[w], cols, r, c, v[0]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[0][i]));
     }
@@ -667,7 +666,7 @@ __global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
     for (int e2 = 0; e2 < E; ++e2) put(((int64_t)e2 * G + gl) * 8, v[e2]);
   } else {
     for (int64_t c = gl * 8; c < ld; c += G * 8) {
-      eight<float>(src, h.rows[w], cols, r, c, vec, v[0]);
+      eight<float>(src, h.rows[w], cols, r, c, v[0]);
       put(c, v[0]);
     }
   }
