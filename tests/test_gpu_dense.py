@@ -378,3 +378,13 @@ def test_the_binding_refuses_other_tensors():
     with pytest.raises(bd.SpcfgError) as err:
         bd.spcfg_dense_forward(big, e(2048, 512), e(2048, 512), None, None, e(2048, 2048), None, None)
     assert err.value.code == -1
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("R,I,O", [(8000, 5, 2000), (2500, 641, 1003), (1500, 1028, 774), (2200, 513, 1021)])
+def test_rows_of_odd_lengths_on_tiles(R, I, O, types):
+    """Ends of rows at every place of eight values, rows shorter than eight, and the same from an address that nothing lies on."""
+    for shift in (0, 1):
+        print("case dense odd", R, I, O, types, shift, flush=True)
+        check_forward(R, I, O, types, "silu", shift=shift)
+        check_backward(R, I, O, types, "silu", shift=shift)
