@@ -134,3 +134,10 @@ def test_the_binding_refuses_host_tensors():
         bd.spcfg_distill_forward(torch.zeros(2, 5, dtype=torch.float64), None, torch.zeros(2, 3), 1.0, None, None, None)
     with pytest.raises(TypeError):
         bd.spcfg_dense_forward(dense(), torch.zeros(4, 8), torch.zeros(8, 8), None, None, torch.zeros(4, 8), None, None)
+
+
+@pytest.mark.parametrize("which", ["forward", "backward", "both"])
+def test_temperatures_without_a_finite_inverse(which):
+    """What the scores are multiplied by, log2(e) / temperature, has to be a finite float."""
+    assert distill(which, tau=4e-39) == ARG
+    assert distill(which, tau=0.0) == ARG
