@@ -236,8 +236,9 @@ int spcfg_rules_backward(int32_t N, int32_t P, int32_t V, const float* log_root,
  *     product: three exact bf16 pieces of each value, or, in large forward products, two fp16 pieces of its row scaled by a
  *     power of two (values below 2^-29 of their row's largest are then good to 2^-51 of that one).  An infinite operand makes
  *     the results that it enters NaN, and one above 3.38e38 may.
- *   in_type BF16 (out_type BF16 or F32): products of the given values accumulated in fp32; the backward pass rounds
- *     grad_y * act'(z) to bf16, the operands' type.
+ *   in_type BF16 (out_type BF16 or F32): products of the given values accumulated in fp32.  The backward pass multiplies
+ *     grad_y * act'(z), a value of fp32, as two bf16 pieces that hold it to 2^-17 (as one where it is a bf16 value); beside two
+ *     pieces an infinite x or W makes the gradients that it enters NaN.
  * Activations and epilogues are computed in fp32 and rounded to the result's type once.
  */
 enum { SPCFG_TYPE_F32 = 0, SPCFG_TYPE_BF16 = 1 };

@@ -98,6 +98,27 @@ template <int N> __device__ __forceinline__ void times_slopes(int act, const flo
   }
 }
 
+// dz = grad_y * act'(z) beside bf16 operands is a 32-bit product: rounded to one bf16 value, 2^-8, it would put as much error into
+// the gradients as their own rounding does (2.3e-3 in relative L2 where that alone makes 1.7e-3).  So it is multiplied as two pieces,
+// hi = bf16(d) and lo = bf16(d - hi), good to 2^-17; in a second product, which matrix cores that wait for operands have room for.
+struct Split2 {
+  uintx4 hi, lo;
+  __device__ __forceinline__ void cut(const float (&d)[8], bool two) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      hi[i] = Split3::pack_rne(d[2 * i], d[2 * i + 1]);
+      if (two) {  // (beside an infinite piece the other is nothing, not inf - inf)
+        const float h0 = __uint_as_float(hi[i] << 16), h1 = __uint_as_float(hi[i] & 0xffff0000u);
+        lo[i] = Split3::pack_rne(fabsf(h0) == INFINITY ? 0.0f : d[2 * i] - h0, fabsf(h1) == INFINITY ? 0.0f : d[2 * i + 1] - h1);
+      }
+    }
+  }
+};
+// how many: one where grad_y is bf16 and its slope 0 or 1, since dz is then a bf16 value itself
+template <typename TI, typename TO> __host__ __device__ constexpr int dz_pieces(int act) {
+  return sizeof(TI) == 4 ? 3 : sizeof(TO) == 2 && (act == SPCFG_ACT_NONE || act == SPCFG_ACT_RELU) ? 1 : 2;
+}
+
 // Everything a layer's kernels take.  R rows, I inputs, O outputs; matrices dense and row-major.
 struct Args {
   int64_t R, I, O;

@@ -7,7 +7,7 @@
 // K in turn, several at a time with everything of theirs in flight, and meet once, in LDS, where the epilogue runs on whole
 // rows of the tile.  Small products are bound by latency: a few trips to memory, a few matrix instructions and one exchange.
 // fp32 operands are cut exactly into three bf16 pieces in registers and multiplied as six piece products (nt::Split3), dz is
-// formed on the way.
+// formed on the way, beside bf16 operands as two bf16 pieces (Split2).
 #include <type_traits>
 
 #include "dense.h"
@@ -29,14 +29,12 @@ template <> struct Pieces<float> {
     s.cut(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]));
   }
   __device__ __forceinline__ void raw(const float (&v)[8]) { set(v); }
+  __device__ __forceinline__ void dz(const float (&v)[8], bool) { set(v); }
 };
 template <> struct Pieces<uint16_t> {
-  uintx4 h;
-  __device__ __forceinline__ void set(const float (&v)[8]) {  // dz is rounded to the operands' type, as W and x are
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = Split3::pack_rne(v[2 * i], v[2 * i + 1]);
-  }
-  __device__ __forceinline__ void raw(const uint16_t (&v)[8]) { __builtin_memcpy(&h, v, 16); }
+  Split2 s;
+  __device__ __forceinline__ void raw(const uint16_t (&v)[8]) { __builtin_memcpy(&s.hi, v, 16); }
+  __device__ __forceinline__ void dz(const float (&v)[8], bool two) { s.cut(v, two); }
 };
 
 // the matrix instruction of T x T: 16 k, resp. 32; lane l holds row l % T of an operand, k = 8 (l / T) .. + 7
@@ -58,7 +56,7 @@ template <> struct Mma<16> {
   }
 };
 template <typename M>
-__device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<float>& b, typename M::Acc& c) {
+__device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<float>& b, bool, typename M::Acc& c) {
   c = M::mul(a.s.lo, b.s.hi, c);
   c = M::mul(a.s.hi, b.s.lo, c);
   c = M::mul(a.s.mid, b.s.mid, c);
@@ -67,8 +65,9 @@ __device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<flo
   c = M::mul(a.s.hi, b.s.hi, c);
 }
 template <typename M>
-__device__ __forceinline__ void product(const Pieces<uint16_t>& a, const Pieces<uint16_t>& b, typename M::Acc& c) {
-  c = M::mul(a.h, b.h, c);
+__device__ __forceinline__ void product(const Pieces<uint16_t>& a, const Pieces<uint16_t>& b, bool two, typename M::Acc& c) {
+  if (two) c = M::mul(a.s.lo, b.s.hi, c);
+  c = M::mul(a.s.hi, b.s.hi, c);
 }
 
 // v[i] = element (row, k + i), i = 0 .. 7, of an operand that runs along k; zero from K on (what is loaded there is the row's last,
@@ -118,7 +117,7 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
   const TI* W = static_cast<const TI*>(g.W);
   const TO* gy = static_cast<const TO*>(g.grad_y);
   const TO* z = static_cast<const TO*>(g.preact_in);
-  const bool slope = g.act != SPCFG_ACT_NONE;
+  const bool slope = g.act != SPCFG_ACT_NONE, two = FORM != FWD && dz_pieces<TI, TO>(g.act) == 2;
 
   typename M::Acc acc;
 #pragma unroll
@@ -173,10 +172,10 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
 #pragma unroll
           for (int e = 0; e < 8; ++e) bsum += d[e];
         }
-        A.set(d);
+        A.dz(d, two);
       }
       B.raw(vb[u]);
-      product<M>(A, B, acc);
+      product<M>(A, B, two, acc);
     }
   }
 

@@ -8,8 +8,10 @@
 //    half the matrix work of the next form.  Without the 2^11 lo would lose bits from 2^-16 of the largest value on.
 //  * fp32 operands of the backward products are cut exactly into three bf16 planes (nt::Split3: hi, mid, lo) and multiplied as
 //    six piece products: these run across rows, whose scales could not be taken out of the sum.
-//  * dz = grad_y * act'(z) is written as one or three planes by the kernel that cuts, which adds up the bias's gradient on the
-//    way (not needed where grad_y is bf16 and there is no activation: dz is grad_y).
+//  * dz = grad_y * act'(z) is written as planes by the kernel that cuts, which adds up the bias's gradient on the way: three of
+//    fp32 operands, as above; with bf16 operands two, hi = bf16(dz) and lo = bf16(dz - hi), dz to 2^-17, multiplied as two piece
+//    products with the other operand's one; one where grad_y is bf16 and its slope 0 or 1, and dz is a bf16 value (none is needed
+//    without an activation: dz is grad_y).
 //  * Each operand runs along k (rows of x and W in the forward product, rows of dz in dx) or across it (W in dx, dz and x in
 //    dW): nothing is transposed in memory.  Tiles go from global memory straight to LDS (16 bytes a lane), a step being
 //    32 or 64 values of k: rows of 64 or 128 bytes along k, with the 16-byte piece XORed with bits 2..3, resp. 1..3 of the
@@ -22,6 +24,8 @@
 // No workgroup waits for another; sums run in an order fixed by the sizes.
 // Bound by the matrix cores on wide layers (bf16 8192^3 1250 TFLOP/s, 8192 x 4096 x 4096 with gelu 241 to 250 us = 1100 to 1140;
 // a library product of that size 1297), by LDS reads on tiles of 128 (700 to 800 TFLOP/s), by latency below some 2e9 products.
+// Backward 2048 x 512 x 10000 from fp32 gradients of bf16 layers: 132 us, of them two planes of dz 29, tiles 87 (two piece
+// products each, 970 TFLOP/s of them), joining parts 5.
 #include <type_traits>
 #include <utility>
 
@@ -61,25 +65,28 @@ __device__ __forceinline__ bf16x8 operand(const uintx4& f) { return __builtin_bi
 __device__ __forceinline__ void tie(Frag& f) { asm volatile("" : "+v"(f.lo), "+v"(f.hi)); }
 __device__ __forceinline__ void tie(uintx4& f) { asm volatile("" : "+v"(f)); }
 
-// PL planes; a tile of BM x BN by WM x WN wavefronts; BK values of k a step; NS steps in LDS.  Two planes lie side by side, 32
-// values of one and the same 32 of the other, so that a step is a whole line of 128 bytes of each row: to loads they are
-// MP = 1 plane of ME = 64 values a step.
-template <int PL_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct Shape {
-  static constexpr int PL = PL_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
+// PA and PB planes of A and B; a tile of BM x BN by WM x WN wavefronts; BK values of k a step; NS steps in LDS.  Two fp16 planes of
+// either (HALVES) lie side by side, 32 values of one and the same 32 of the other, so that a step is a whole line of 128 bytes of
+// each row: to loads they are one plane (MA = MB = 1) of ME = 64 values a step.
+template <int PA_, int PB_, int BM_, int BN_, int WM_, int WN_, int BK_, int NS_> struct Shape {
+  static constexpr int PA = PA_, PB = PB_, BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, NS = NS_;
+  static constexpr bool HALVES = PA == 2 && PB == 2;
   static constexpr int NW = WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN);
-  static constexpr int MP = PL == 2 ? 1 : PL, ME = PL == 2 ? 2 * BK : BK;
+  static constexpr int MA = HALVES ? 1 : PA, MB = HALVES ? 1 : PB, ME = HALVES ? 2 * BK : BK;
   static constexpr int RB = 2 * ME;                   // bytes of a row along k
   static constexpr int PTA = BM * RB, PTB = BN * RB;  // bytes of one plane's tile
-  static constexpr int STAGE = MP * (PTA + PTB);
+  static constexpr int TILE_B = MA * PTA, STAGE = TILE_B + MB * PTB;  // where B's tiles begin, and a step's bytes
   static constexpr int LA = PTA / 1024, LB = PTB / 1024;  // 1 KB loads of a plane's tile
-  static constexpr int NDA = MP * LA / NW, ND = MP * (LA + LB) / NW;  // of a wavefront and step, the first NDA of A
+  static constexpr int NDA = MA * LA / NW, ND = NDA + MB * LB / NW;  // of a wavefront and step, the first NDA of A
   static constexpr int CH = BK / 16;                  // chunks of 16 k in a step
-  static constexpr int NM = (PL == 3 ? 6 : PL == 2 ? 3 : 1) * MI * NI;  // matrix instructions of a chunk
-  static constexpr int NA = PL == 2 ? 2 : 1;          // sums: fp16 planes keep the small products apart
+  static constexpr int PP = HALVES ? 3 : PA == 3 ? 6 : PA;  // piece products
+  static constexpr int NM = PP * MI * NI;             // matrix instructions of a chunk
+  static constexpr int NA = HALVES ? 2 : 1;           // sums: fp16 planes keep the small products apart
   static constexpr int kLds = NS * STAGE;
+  static_assert(PA == PB ? PA <= 3 : PA == 2 && PB == 1, "one, two or three planes of both, or two of A and one of B");
   static_assert(LA % NW == 0 && LB % NW == 0, "loads of a plane's tile are dealt evenly");
   static_assert((BM < 128) == (BN < 128), "panels across k are as wide for both operands");
-  static_assert((ME == 32 || ME == 64) && (PL != 2 || BK == 32) && NS >= 2 && ND * (NS - 1) < 64, "");
+  static_assert((ME == 32 || ME == 64) && (!HALVES || BK == 32) && CH % 2 == 0 && NS >= 2 && ND * (NS - 1) < 64, "");
 };
 
 #define SPCFG_SB __builtin_amdgcn_sched_barrier(0);
@@ -113,8 +120,9 @@ __device__ __forceinline__ void add_floats(const float* p, float (&s)[8], int64_
 template <typename S, typename TI, typename TO, int FORM>
 __device__ __forceinline__ void tile_product(const Args& g, const Product& p, unsigned b, unsigned all, unsigned char* lds) {
   constexpr bool TA = FORM == DW, TB = FORM != FWD;
-  constexpr int PL = S::PL, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, CH = S::CH, MP = S::MP, ME = S::ME;
-  static_assert(PL != 2 || FORM == FWD, "two planes run along k");
+  constexpr int PA = S::PA, PB = S::PB, MI = S::MI, NI = S::NI, ND = S::ND, NM = S::NM, NS = S::NS, CH = S::CH, ME = S::ME;
+  constexpr bool HALVES = S::HALVES;
+  static_assert(!HALVES || FORM == FWD, "fp16 planes run along k");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % S::WM, wn = wave / S::WM;
@@ -149,7 +157,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     constexpr bool isA = jv < S::NDA;
     constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
     const int q = wave + e0 % per;
-    e_lds[jv] = (unsigned)((isA ? plane * S::PTA : MP * S::PTA + plane * S::PTB) + q * 1024);
+    e_lds[jv] = (unsigned)((isA ? plane * S::PTA : S::TILE_B + plane * S::PTB) + q * 1024);
     const int64_t ld = isA ? p.lda : p.ldb, len = isA ? p.M : p.N, o0 = isA ? m0 : n0;
     if constexpr (isA ? TA : TB) {
       const int64_t col = min(o0 + q / QA * PW + c_ac, (len + 7) / 8 * 8 - 8) - o0;  // (never before the tile: o0 < len)
@@ -160,14 +168,16 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     }
   });
   const int64_t step_a = TA ? 2 * ME * p.lda : 2 * ME, step_b = TB ? 2 * ME * p.ldb : 2 * ME;  // bytes a step
-  const unsigned char* base[2][MP];  // of the step that is loaded next
-  static_for<0, MP>([&](auto pl) {
+  const unsigned char* base[S::MA + S::MB];  // of the step that is loaded next; A's planes, then B's
+  static_for<0, S::MA + S::MB>([&](auto pl) {
     constexpr int v = decltype(pl)::value;
-    base[0][v] = reinterpret_cast<const unsigned char*>(p.A + v * p.plane_a + (TA ? m0 : m0 * p.lda)) + k0 * step_a;
-    base[1][v] = reinterpret_cast<const unsigned char*>(p.B + v * p.plane_b + (TB ? n0 : n0 * p.ldb)) + k0 * step_b;
+    if constexpr (v < S::MA)
+      base[v] = reinterpret_cast<const unsigned char*>(p.A + v * p.plane_a + (TA ? m0 : m0 * p.lda)) + k0 * step_a;
+    else
+      base[v] = reinterpret_cast<const unsigned char*>(p.B + (v - S::MA) * p.plane_b + (TB ? n0 : n0 * p.ldb)) + k0 * step_b;
     // (opaque: otherwise they are computed anew from kernel arguments inside the loop, and waiting for those waits for
     // operand reads as well)
-    asm volatile("" : "+s"(base[0][v]), "+s"(base[1][v]));
+    asm volatile("" : "+s"(base[v]));
   });
   int64_t by_a = step_a, by_b = step_b;
   asm volatile("" : "+s"(by_a), "+s"(by_b));
@@ -175,14 +185,11 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     constexpr int jv = decltype(j)::value;
     constexpr bool isA = jv < S::NDA;
     constexpr int plane = S::NW * (isA ? jv : jv - S::NDA) / (isA ? S::LA : S::LB);
-    dma16(base[isA ? 0 : 1][plane] + e_off[jv], lds0 + stage + e_lds[jv]);
+    dma16(base[isA ? plane : S::MA + plane] + e_off[jv], lds0 + stage + e_lds[jv]);
   };
   auto advance = [&]() {
 #pragma unroll
-    for (int v = 0; v < MP; ++v) {
-      base[0][v] += by_a;
-      base[1][v] += by_b;
-    }
+    for (int v = 0; v < S::MA + S::MB; ++v) base[v] += v < S::MA ? by_a : by_b;
   };
   // the last step of all where k ends inside it: what lies beyond reads as zero
   const int last_left = (int)(p.K - (int64_t)(p.steps - 1) * ME);  // values of the last step, 1 .. ME
@@ -194,7 +201,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
       constexpr int per = isA ? S::LA : S::LB, e0 = S::NW * (isA ? jv : jv - S::NDA), plane = e0 / per;
       const int q = wave + e0 % per;
       const int k = (isA ? TA : TB) ? RP * (q % QA) + r_ac : 8 * (ME == 32 ? c_al : c_al ^ (((RL * q + r_al) >> 1) & 7));
-      const unsigned char* at = base[isA ? 0 : 1][plane] + e_off[jv];
+      const unsigned char* at = base[isA ? plane : S::MA + plane] + e_off[jv];
       dma16(k < last_left ? at : reinterpret_cast<const unsigned char*>(&g_zeros), lds0 + stage + e_lds[jv]);
     });
   };
@@ -221,51 +228,48 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
 #pragma unroll
       for (int f = 0; f < NI; ++f) {
         const int blk = wn * NI + f;
-        fb[f] = MP * S::PTA + ac + (unsigned)(blk / PB * (ME * 2 * PW) + ((blk % PB) ^ key) * 64);
+        fb[f] = S::TILE_B + ac + (unsigned)(blk / PB * (ME * 2 * PW) + ((blk % PB) ^ key) * 64);
       }
     } else {
-      fb[0] = MP * S::PTA + al + (unsigned)(wn * NI * 32 * S::RB);
+      fb[0] = S::TILE_B + al + (unsigned)(wn * NI * 32 * S::RB);
     }
   }
   using FA = typename std::conditional<TA, Frag, uintx4>::type;
   using FB = typename std::conditional<TB, Frag, uintx4>::type;
-  struct Chunk { FA a[PL][MI]; FB b[PL][NI]; };
+  struct Chunk { FA a[PA][MI]; FB b[PB][NI]; };
   Chunk X, Y;
   // fragment r of a chunk: planes of A, then of B
-  constexpr int NF = PL * (MI + NI);
+  constexpr int NF = PA * MI + PB * NI;
   auto read_one = [&](Chunk& F, auto r, unsigned stage, auto chunk) {
     constexpr int rv = decltype(r)::value, cv = decltype(chunk)::value;
-    if constexpr (rv < PL * MI) {
+    if constexpr (rv < PA * MI) {
       constexpr int pl = rv / MI, f = rv % MI;
       if constexpr (TA) {
         const unsigned at = lds0 + stage + fa[f];
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].lo) : "v"(at), "n"(pl * S::PTA + cv * 32 * PW));
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.a[pl][f].hi) : "v"(at), "n"(pl * S::PTA + cv * 32 * PW + 8 * PW));
       } else {
-        const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTA) + f * 32 * S::RB));
+        const unsigned at = lds0 + stage + (fa[0] ^ (cv * 32u + (HALVES ? pl * 64u : 0u)));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.a[pl][f]) : "v"(at), "n"((HALVES ? 0 : pl * S::PTA) + f * 32 * S::RB));
       }
     } else {
-      constexpr int pl = (rv - PL * MI) / NI, f = (rv - PL * MI) % NI;
+      constexpr int pl = (rv - PA * MI) / NI, f = (rv - PA * MI) % NI;
       if constexpr (TB) {
         const unsigned at = lds0 + stage + fb[f];
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].lo) : "v"(at), "n"(pl * S::PTB + cv * 32 * PW));
         asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(F.b[pl][f].hi) : "v"(at), "n"(pl * S::PTB + cv * 32 * PW + 8 * PW));
       } else {
-        const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u + (PL == 2 ? pl * 64u : 0u)));
-        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"((PL == 2 ? 0 : pl * S::PTB) + f * 32 * S::RB));
+        const unsigned at = lds0 + stage + (fb[0] ^ (cv * 32u + (HALVES ? pl * 64u : 0u)));
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(F.b[pl][f]) : "v"(at), "n"((HALVES ? 0 : pl * S::PTB) + f * 32 * S::RB));
       }
     }
   };
   auto wait_reads = [&](Chunk& F) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int pl = 0; pl < PL; ++pl) {
+    for (int f = 0; f < PA * MI; ++f) tie(F.a[f / MI][f % MI]);
 #pragma unroll
-      for (int f = 0; f < MI; ++f) tie(F.a[pl][f]);
-#pragma unroll
-      for (int f = 0; f < NI; ++f) tie(F.b[pl][f]);
-    }
+    for (int f = 0; f < PB * NI; ++f) tie(F.b[f / NI][f % NI]);
   };
   floatx16 acc[S::NA][MI][NI];
 #pragma unroll
@@ -278,13 +282,13 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
         for (int v = 0; v < 16; ++v) acc[a][i][j][v] = 0.0f;
   auto mfma_one = [&](Chunk& F, auto i) {
     constexpr int pp = decltype(i)::value / (MI * NI), rem = decltype(i)::value % (MI * NI), mi = rem / NI, ni = rem % NI;
-    if constexpr (PL == 2) {  // lo*hi and hi*lo into the second sum, hi*hi into the first (0 hi, 1 lo)
+    if constexpr (HALVES) {  // lo*hi and hi*lo into the second sum, hi*hi into the first (0 hi, 1 lo)
       constexpr int pa = pp == 0 ? 1 : 0, pb = pp == 1 ? 1 : 0, a = pp == 2 ? 0 : 1;
       acc[a][mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, F.a[pa][mi]),
                                                               __builtin_bit_cast(halfx8, F.b[pb][ni]), acc[a][mi][ni], 0, 0, 0);
-    } else {  // three planes: lo*hi, hi*lo, mid*mid, mid*hi, hi*mid, hi*hi (0 hi, 1 mid, 2 lo)
-      constexpr int pa = PL == 1 ? 0 : pp == 0 ? 2 : (pp == 2 || pp == 3 ? 1 : 0);
-      constexpr int pb = PL == 1 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
+    } else {  // three planes: lo*hi, hi*lo, mid*mid, mid*hi, hi*mid, hi*hi (0 hi, 1 mid, 2 lo); two of A: lo*B, hi*B (0 hi, 1 lo)
+      constexpr int pa = PA < 3 ? PA - 1 - pp : pp == 0 ? 2 : (pp == 2 || pp == 3 ? 1 : 0);
+      constexpr int pb = PA < 3 ? 0 : pp == 1 ? 2 : (pp == 2 || pp == 4 ? 1 : 0);
       acc[0][mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(F.a[pa][mi]), operand(F.b[pb][ni]), acc[0][mi][ni], 0, 0, 0);
     }
   };
@@ -381,7 +385,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
     return S::NA == 2 ? fmaf(acc[S::NA - 1][mi][ni][v], 0x1p-11f, acc[0][mi][ni][v]) : acc[0][mi][ni][v];
   };
   int down[8];
-  if (PL == 2) {
+  if (HALVES) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) down[u] = p.exp_b[min(c + u, p.N - 1)];
   }
@@ -403,7 +407,7 @@ __device__ __forceinline__ void tile_product(const Args& g, const Product& p, un
         s[u + 4] = from[4 - odd + u];
       }
       if (m >= p.M || c >= p.N) continue;
-      if (PL == 2) {
+      if (HALVES) {
         const int e = p.exp_a[m];
 #pragma unroll
         for (int u = 0; u < 8; ++u) s[u] = __builtin_amdgcn_ldexpf(s[u], -(e + down[u]));
@@ -498,10 +502,19 @@ __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t plane, const f
   *reinterpret_cast<uintx4*>(dst + 2 * plane) = s.lo;
 }
 __device__ __forceinline__ void put_planes(uint16_t* dst, int64_t, const float (&v)[8], uint16_t) {
-  uintx4 h;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = Split3::pack_rne(v[2 * i], v[2 * i + 1]);
-  *reinterpret_cast<uintx4*>(dst) = h;
+  Split2 s;
+  s.cut(v, false);
+  *reinterpret_cast<uintx4*>(dst) = s.hi;
+}
+// dz as planes of the operands' type
+__device__ __forceinline__ void put_dz(uint16_t* dst, int64_t plane, const float (&v)[8], bool, float) {
+  put_planes(dst, plane, v, 0.0f);
+}
+__device__ __forceinline__ void put_dz(uint16_t* dst, int64_t plane, const float (&v)[8], bool two, uint16_t) {
+  Split2 s;
+  s.cut(v, two);
+  *reinterpret_cast<uintx4*>(dst) = s.hi;
+  if (two) *reinterpret_cast<uintx4*>(dst + plane) = s.lo;
 }
 
 // eight values of a row from column c on, zero outside the matrix (where the nearest ones inside are loaded: no load hangs on a
@@ -557,6 +570,7 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
   const int64_t r1 = min(rows32, (int64_t)(part + 1) * span);
   const TO* gy = static_cast<const TO*>(g.grad_y);
   const TO* z = static_cast<const TO*>(g.preact_in);
+  const bool two = dz_pieces<TI, TO>(g.act) == 2;
   float s[8] = {};
   if (c < ld) {
     // (four rows' loads in flight)
@@ -572,7 +586,7 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (dst && r0 + 4 * u < r1) put_planes(dst + (r0 + 4 * u) * ld + c, rows32 * ld, d[u], TI());
+        if (dst && r0 + 4 * u < r1) put_dz(dst + (r0 + 4 * u) * ld + c, rows32 * ld, d[u], two, TI());
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += d[u][i];
       }
@@ -688,7 +702,9 @@ struct Choice { int t, sa, sb; double us; };
 // workgroup where all run at once, as their mean with half the longest on top where they do not; splitting costs a launch
 // more (6 us) and partial tiles written and read again at 4 TB/s.  Of the lengths that cut the longer product into 1, 2, 3, ... shares the best is taken.
 // Measured (us): 4096 x 512 x 512 in fp32 (128 tiles of 128 x 128, 16 steps) in two 37, in one 30, on 64 x 64 24;
-// bf16 8192 x 4096 x 4096 on 256 x 256 241, on 128 x 128 320; 2048 x 512 x 10000 61, 43; 512^3 on 128 x 128 9.7, on 64 x 64 6.9.
+// bf16 8192 x 4096 x 4096 on 256 x 256 241, on 128 x 128 320; 2048 x 512 x 10000 61, 43; 512^3 on 128 x 128 9.7, on 64 x 64 6.9;
+// backward with dz in two pieces, on 256, 128 and 64: 8192 x 2048 x 2048 289, 326, 411; 2048 x 512 x 10000 148, 133, 170;
+// 512^3 30, 15.5, 12.
 void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Choice* best) {
   auto work = [&](const int64_t (&d)[3]) {
     return Work{d[2] ? tiles(d[0], g.t) * tiles(d[1], g.t) : 0, tiles(d[2], g.bk)};
@@ -716,7 +732,7 @@ void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Cho
 struct Plan {
   bool on;                 // whether the layer takes tiled products at all
   bool cut;                // x and W as planes (fp32, or rows that do not lie on 16 bytes)
-  bool dz;                 // dz as planes
+  int dz;                  // planes of dz that are written; 0: dz is grad_y
   int64_t x, w, z;         // elements of one plane of x, W, dz
   int span, parts;         // rows of a part of the bias's gradient
   Choice c;
@@ -730,7 +746,8 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   const bool fp32 = in_type == SPCFG_TYPE_F32;
   const int pl = fp32 ? 3 : 1;
   p.cut = fp32 || I % 8 != 0;
-  p.dz = what != FORWARD && (fp32 || out_type == SPCFG_TYPE_F32 || act != SPCFG_ACT_NONE || O % 8 != 0);
+  const int pz = fp32 ? 3 : out_type == SPCFG_TYPE_F32 ? dz_pieces<uint16_t, float>(act) : dz_pieces<uint16_t, uint16_t>(act);
+  p.dz = what != FORWARD && (pz > 1 || act != SPCFG_ACT_NONE || O % 8 != 0) ? pz : 0;
   p.x = up32(R) * up32(I);
   p.w = up32(O) * up32(I);
   p.z = up32(R) * up32(O);
@@ -749,6 +766,10 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   } else if (fp32) {
     consider(Tiling{64, 32, 512, 8, 5, 0.45, 0.39}, da, db, &p.c);
     consider(Tiling{128, 32, 256, 6, 5, 1.2, 1.25}, da, db, &p.c);
+  } else if (p.dz == 2) {  // two piece products
+    consider(Tiling{64, 64, 512, 4, 5, 0.4, 0.3}, da, db, &p.c);
+    consider(Tiling{128, 64, 512, 4, 5, 0.9, 0.8}, da, db, &p.c);
+    consider(Tiling{256, 64, 256, 10, 15, 2, 2.5}, da, db, &p.c);
   } else {
     consider(Tiling{64, 64, 512, 4, 5, 0.3, what == FORWARD ? 0.3 : 0.25}, da, db, &p.c);
     consider(Tiling{128, 64, 512, 3, 5, 0.75, 0.67}, da, db, &p.c);
@@ -759,7 +780,7 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   double bytes = 0;
   const double a_value = fp32 && what == FORWARD ? 8 : si * 2.5;
   if (p.cut) bytes += a_value * ((what != BACK_X ? (double)R * I : 0) + (what != BACK_W ? (double)O * I : 0));
-  if (what != FORWARD) bytes += (double)R * O * ((act ? 2 : 1) * so + (p.dz ? 2 * pl : 0));
+  if (what != FORWARD) bytes += (double)R * O * ((act ? 2 : 1) * so + 2 * p.dz);
   const double us = p.c.us + (bytes > 0 ? 3 + bytes / 4e6 : 0);
   p.on = us < direct_us(R, I, O, in_type, what);
   if (!p.on) return p;
@@ -768,7 +789,7 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   p.off_x = take(p.cut ? (size_t)p.x * 2 * pl : 0);
   p.off_w = take(p.cut ? (size_t)p.w * 2 * pl : 0);
   p.off_e = take(fp32 && what == FORWARD ? (size_t)(R + O) * 4 : 0);
-  p.off_z = take(p.dz ? (size_t)p.z * 2 * pl : 0);
+  p.off_z = take((size_t)p.z * 2 * p.dz);
   p.off_sums = take(what != FORWARD ? (size_t)p.parts * O * 4 : 0);
   p.off_pa = take(p.c.sa > 1 ? (size_t)p.c.sa * da[0] * da[1] * 4 : 0);
   p.off_pb = take(p.c.sb > 1 ? (size_t)p.c.sb * db[0] * db[1] * 4 : 0);
@@ -806,20 +827,26 @@ void launch_backward(const Args& a, Product x, Product w, int sx, int sw, const 
   if (jx + jw) hipLaunchKernelGGL((k_dense_backward_join<TI, TO>), dim3(jx + jw), dim3(256), 0, st, a, x, w, jx);
 }
 
-// The shapes of a type's products: tiles of 64, 128 and (bf16) 256; at 128 and 256 two wavefronts per SIMD and workgroup, one
-// issuing while the other waits
-template <typename TI, bool BACKWARD> struct Shapes {
-  using T64 = Shape<1, 64, 64, 2, 2, 64, 4>;
-  using T128 = Shape<1, 128, 128, 2, 4, 64, 2>;
-  using T256 = Shape<1, 256, 256, 2, 4, 64, 2>;
+// The shapes of the products, by the planes of their operands: tiles of 64, 128 and (bf16) 256; at 128 and 256 two wavefronts per
+// SIMD and workgroup, one issuing while the other waits
+template <int PA, int PB> struct Shapes;
+template <> struct Shapes<1, 1> {
+  using T64 = Shape<1, 1, 64, 64, 2, 2, 64, 4>;
+  using T128 = Shape<1, 1, 128, 128, 2, 4, 64, 2>;
+  using T256 = Shape<1, 1, 256, 256, 2, 4, 64, 2>;
 };
-template <> struct Shapes<float, false> {
-  using T64 = Shape<2, 64, 64, 2, 2, 32, 4>;
-  using T128 = Shape<2, 128, 128, 2, 4, 32, 2>;
+template <> struct Shapes<2, 1> {
+  using T64 = Shape<2, 1, 64, 64, 2, 2, 64, 3>;
+  using T128 = Shape<2, 1, 128, 128, 2, 4, 32, 3>;  // (2048 x 512 x 10000 133 us, with two steps of 64 151, two of 32 148)
+  using T256 = Shape<2, 1, 256, 256, 2, 4, 32, 3>;
 };
-template <> struct Shapes<float, true> {
-  using T64 = Shape<3, 64, 64, 2, 2, 32, 3>;
-  using T128 = Shape<3, 128, 128, 2, 4, 32, 3>;
+template <> struct Shapes<2, 2> {
+  using T64 = Shape<2, 2, 64, 64, 2, 2, 32, 4>;
+  using T128 = Shape<2, 2, 128, 128, 2, 4, 32, 2>;
+};
+template <> struct Shapes<3, 3> {
+  using T64 = Shape<3, 3, 64, 64, 2, 2, 32, 3>;
+  using T128 = Shape<3, 3, 128, 128, 2, 4, 32, 3>;
 };
 
 template <typename TI, typename TO>
@@ -854,7 +881,7 @@ void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
     q.A = static_cast<const uint16_t*>(a.x); q.B = static_cast<const uint16_t*>(a.W);
     q.lda = q.ldb = q.K = a.I;
   }
-  using S = Shapes<TI, false>;
+  using S = typename std::conditional<std::is_same<TI, float>::value, Shapes<2, 2>, Shapes<1, 1>>::type;
   if (p.c.t == 64) return launch_forward<typename S::T64, TI, TO>(a, q, p.c.sa, st);
   if constexpr (!std::is_same<TI, float>::value) {
     if (p.c.t == 256) return launch_forward<typename S::T256, TI, TO>(a, q, p.c.sa, st);
@@ -862,7 +889,7 @@ void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   launch_forward<typename S::T128, TI, TO>(a, q, p.c.sa, st);
 }
 
-template <typename TI, typename TO>
+template <typename S, typename TI, typename TO>
 void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   const uint16_t *x = static_cast<const uint16_t*>(a.x), *W = static_cast<const uint16_t*>(a.W);
   const uint16_t* z = static_cast<const uint16_t*>(a.grad_y);
@@ -897,7 +924,6 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   dw.M = a.O; dw.N = a.I;
   dw.K = padded ? up32(a.R) : a.R;
   dw.partial = reinterpret_cast<float*>(ws + p.off_pb);
-  using S = Shapes<TI, true>;
   if (p.c.t == 64) return launch_backward<typename S::T64, TI, TO>(a, dx, dw, p.c.sa, p.c.sb, r.sums, p.parts, st);
   if constexpr (!std::is_same<TI, float>::value) {
     if (p.c.t == 256) return launch_backward<typename S::T256, TI, TO>(a, dx, dw, p.c.sa, p.c.sb, r.sums, p.parts, st);
@@ -930,9 +956,10 @@ bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStrea
   const Plan p = plan_of(a.R, a.I, a.O, in_type, out_type, a.act, (a.grad_x ? BACK_X : 0) | (a.grad_W ? BACK_W : 0));
   if (!p.on || (!p.cut && (!on16(a.x) || !on16(a.W))) || (!p.dz && !on16(a.grad_y))) return false;
   char* w = static_cast<char*>(ws);
-  if (in_type == SPCFG_TYPE_F32) backward<float, float>(a, p, w, st);
-  else if (out_type == SPCFG_TYPE_F32) backward<uint16_t, float>(a, p, w, st);
-  else backward<uint16_t, uint16_t>(a, p, w, st);
+  if (in_type == SPCFG_TYPE_F32) backward<Shapes<3, 3>, float, float>(a, p, w, st);
+  else if (out_type == SPCFG_TYPE_F32) backward<Shapes<2, 1>, uint16_t, float>(a, p, w, st);
+  else if (p.dz == 2) backward<Shapes<2, 1>, uint16_t, uint16_t>(a, p, w, st);
+  else backward<Shapes<1, 1>, uint16_t, uint16_t>(a, p, w, st);
   return true;
 }
 
