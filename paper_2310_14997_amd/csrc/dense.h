@@ -235,6 +235,8 @@ __device__ __forceinline__ void store_bias(const Args& g, int64_t m, float s) {
   *o = from_float<TI>(s);
 }
 
+constexpr unsigned kMostWorkgroups = 1u << 22;  // of a launch, of up to 512 threads each
+
 inline bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // what a call computes: FORWARD, or of the backward pass dx, dW or both

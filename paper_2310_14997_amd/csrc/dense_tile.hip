@@ -424,11 +424,18 @@ template <int NW, typename TI>
 __device__ __forceinline__ void bias_sums(const Args& g, const float* __restrict__ part, int parts, unsigned block, float* red) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = (int64_t)block * 64 + lane;
-  float s = 0.0f;
+  constexpr int U = 8;  // sums of a thread: as many loads in flight, and shorter runs
+  float f[U] = {};
   if (c < g.O) {
-#pragma unroll 4
-    for (int q = wave; q < parts; q += NW) s += part[(int64_t)q * g.O + c];
+    for (int q = wave; q < parts; q += U * NW) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = part[(int64_t)min(q + u * NW, parts - 1) * g.O + c];
+#pragma unroll
+      for (int u = 0; u < U; ++u) f[u] += q + u * NW < parts ? v[u] : 0.0f;
+    }
   }
+  float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
   red[wave * 64 + lane] = s;
   __syncthreads();
   if (wave == 0 && c < g.O) {
@@ -540,22 +547,24 @@ __device__ __forceinline__ void eight(const T* __restrict__ src, int64_t rows, i
   for (int i = 0; i < 8; ++i) v[i] = r < rows && c + i < cols ? to_float<T>(x[i]) : 0.0f;
 }
 
-// Planes of one matrix, eight values a thread.
+// Planes of one matrix, eight values a thread at a time, by `blocks` workgroups.
 template <typename T>
-__device__ __forceinline__ void cut(const T* __restrict__ src, uint16_t* __restrict__ dst, int64_t rows, int64_t cols, unsigned block) {
-  const int64_t ld = (cols + 31) / 32 * 32, rows32 = (rows + 31) / 32 * 32, e = ((int64_t)block * 256 + threadIdx.x) * 8;
-  if (e >= rows32 * ld) return;
-  int64_t r, c;
-  if (e < ((int64_t)1 << 31)) {  // (a division in 32 bits is far cheaper)
-    r = (unsigned)e / (unsigned)ld;
-    c = (unsigned)e - (unsigned)r * (unsigned)ld;
-  } else {
-    r = e / ld;
-    c = e - r * ld;
+__device__ __forceinline__ void cut(const T* __restrict__ src, uint16_t* __restrict__ dst, int64_t rows, int64_t cols, unsigned block,
+                                    unsigned blocks) {
+  const int64_t ld = (cols + 31) / 32 * 32, rows32 = (rows + 31) / 32 * 32;
+  for (int64_t e = ((int64_t)block * 256 + threadIdx.x) * 8; e < rows32 * ld; e += (int64_t)blocks * (256 * 8)) {
+    int64_t r, c;
+    if (e < ((int64_t)1 << 31)) {  // (a division in 32 bits is far cheaper)
+      r = (unsigned)e / (unsigned)ld;
+      c = (unsigned)e - (unsigned)r * (unsigned)ld;
+    } else {
+      r = e / ld;
+      c = e - r * ld;
+    }
+    float v[8];
+    eight<T>(src, rows, cols, r, c, v);
+    put_planes(dst + e, rows32 * ld, v, T());
   }
-  float v[8];
-  eight<T>(src, rows, cols, r, c, v);
-  put_planes(dst + e, rows32 * ld, v, T());
 }
 
 // dz = grad_y * act'(z) in planes (where dst is given) and, part by part of the rows, its sums over them (where sums is): 512
@@ -585,11 +594,10 @@ __device__ __forceinline__ void make_dz(const Args& g, uint16_t* __restrict__ ds
         for (int u = 0; u < 4; ++u) times_slopes<8>(g.act, y[u], d[u]);
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 4; ++u)
         if (dst && r0 + 4 * u < r1) put_dz(dst + (r0 + 4 * u) * ld + c, rows32 * ld, d[u], two, TI());
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += d[u][i];
-      }
+      for (int i = 0; i < 8; ++i) s[i] += (d[0][i] + d[1][i]) + (d[2][i] + d[3][i]);
     }
   }
   if (!sums) return;
@@ -612,15 +620,15 @@ struct Prepare {
   uint16_t *dz, *x, *W;
   float* sums;
   int span;
-  unsigned col_blocks, blocks_z, blocks_x;  // workgroups of each, W's the rest
+  unsigned col_blocks, blocks_z, blocks_x, blocks_W;  // workgroups of each
 };
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(256) k_dense_prepare(Args g, Prepare q) {
   __shared__ float red[3][512];
   unsigned b = blockIdx.x;
   if (b < q.blocks_z) make_dz<TI, TO>(g, q.dz, q.sums, q.span, q.col_blocks, b, red);
-  else if ((b -= q.blocks_z) < q.blocks_x) cut<TI>(static_cast<const TI*>(g.x), q.x, g.R, g.I, b);
-  else cut<TI>(static_cast<const TI*>(g.W), q.W, g.O, g.I, b - q.blocks_x);
+  else if ((b -= q.blocks_z) < q.blocks_x) cut<TI>(static_cast<const TI*>(g.x), q.x, g.R, g.I, b, q.blocks_x);
+  else cut<TI>(static_cast<const TI*>(g.W), q.W, g.O, g.I, b - q.blocks_x, q.blocks_W);
 }
 
 // fp16 planes of the rows of x and W and the powers of two that they are scaled by.  A group of `group` lanes (a power of two, eight
@@ -688,6 +696,13 @@ __global__ void __launch_bounds__(256) k_dense_halves(Halves h) {
 
 // ---- which form, and what it needs -----------------------------------------------------------------------------------------
 int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
+// workgroups that cut a matrix of `n` values
+unsigned cut_blocks(int64_t n) {
+  const int64_t b = tiles(n / 8, 256);
+  return b < (int64_t)kMostWorkgroups ? (unsigned)b : kMostWorkgroups;
+}
+// The most of k that one sum runs over, 2^12 matrix instructions one behind the other: longer ones are split whatever that costs.
+constexpr int kLongestSum = 1 << 16;
 
 // A product as tiles that go through all of k: `n` of them, of `steps` steps.
 struct Work { int64_t n, steps; };
@@ -711,11 +726,15 @@ void consider(const Tiling& g, const int64_t (&a)[3], const int64_t (&b)[3], Cho
   };
   const Work wa = work(a), wb = work(b);
   const int64_t longer = wb.steps > wa.steps ? wb.steps : wa.steps;
-  for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+  for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
     if (s > 1 && longer < (int64_t)s * g.least) break;
+    if (s > 32 && tiles(longer, 32) <= kLongestSum / g.bk) break;
+    if (tiles(longer, s) > kLongestSum / g.bk) continue;
     const int64_t len = tiles(longer, s), pa = wa.n ? tiles(wa.steps, (int)len) : 0;
     const int64_t pb = wb.n ? tiles(wb.steps, (int)len) : 0;
-    const double wgs = (double)(wa.n * pa + wb.n * pb), here = (wgs < g.room ? wgs : g.room) / 256;
+    const double wgs = (double)(wa.n * pa + wb.n * pb);
+    if (wgs > kMostWorkgroups) continue;
+    const double here = (wgs < g.room ? wgs : g.room) / 256;
     const double step = here * g.busy > g.wait ? here * g.busy : g.wait;
     const double ta = pa ? g.start + step * tiles(wa.steps, (int)pa) : 0;
     const double tb = pb ? g.start + step * tiles(wb.steps, (int)pb) : 0;
@@ -741,8 +760,8 @@ struct Plan {
 
 Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act, int what) {
   Plan p{};
-  const int64_t most = 1 << 22;  // offsets inside a tile (256 rows, or 64 rows across k) fit 32 bits
-  if (R < 1 || R >= most || I >= most || O >= most) return p;
+  const int64_t most = 1 << 22;  // rows that long have offsets inside a tile (256 rows, or 64 across k) of more than 32 bits
+  if (R < 1 || I >= most || O >= most) return p;
   const bool fp32 = in_type == SPCFG_TYPE_F32;
   const int pl = fp32 ? 3 : 1;
   p.cut = fp32 || I % 8 != 0;
@@ -754,6 +773,7 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
   const int64_t cb = tiles(up32(O), 512);
   int64_t span = (up32(R) * cb / 1024 + 15) / 16 * 16;  // about 1024 workgroups, 16 rows at a time
   if (span < 16) span = 16;
+  if (span > 2048) span = 2048;  // (128 additions one behind the other)
   p.span = (int)span;
   p.parts = (int)tiles(up32(R), p.span);
   const int64_t none[3] = {0, 0, 0}, f[3] = {R, O, I}, x[3] = {R, I, O}, w[3] = {O, I, R};
@@ -873,8 +893,9 @@ void forward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
     Prepare r{};
     r.x = reinterpret_cast<uint16_t*>(ws + p.off_x);
     r.W = reinterpret_cast<uint16_t*>(ws + p.off_w);
-    r.blocks_x = (unsigned)tiles(p.x / 8, 256);
-    hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(r.blocks_x + (unsigned)tiles(p.w / 8, 256)), dim3(256), 0, st, a, r);
+    r.blocks_x = cut_blocks(p.x);
+    r.blocks_W = cut_blocks(p.w);
+    hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(r.blocks_x + r.blocks_W), dim3(256), 0, st, a, r);
     q.A = r.x; q.B = r.W;
     q.lda = q.ldb = q.K = up32(a.I);
   } else {
@@ -895,12 +916,11 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
   const uint16_t* z = static_cast<const uint16_t*>(a.grad_y);
   int64_t ldi = a.I, ldo = a.O;
   Prepare r{};
-  unsigned blocks_w = 0;
   if (p.cut) {
     r.x = reinterpret_cast<uint16_t*>(ws + p.off_x);
     r.W = reinterpret_cast<uint16_t*>(ws + p.off_w);
-    if (a.grad_W) r.blocks_x = (unsigned)tiles(p.x / 8, 256);
-    if (a.grad_x) blocks_w = (unsigned)tiles(p.w / 8, 256);
+    if (a.grad_W) r.blocks_x = cut_blocks(p.x);
+    if (a.grad_x) r.blocks_W = cut_blocks(p.w);
     x = r.x; W = r.W; ldi = up32(a.I);
   }
   if (a.grad_bias) r.sums = reinterpret_cast<float*>(ws + p.off_sums);
@@ -910,7 +930,7 @@ void backward(const Args& a, const Plan& p, char* ws, hipStream_t st) {
     r.col_blocks = (unsigned)tiles(up32(a.O), 512);
     r.blocks_z = r.col_blocks * p.parts;
   }
-  const unsigned n = r.blocks_z + r.blocks_x + blocks_w;
+  const unsigned n = r.blocks_z + r.blocks_x + r.blocks_W;
   if (n) hipLaunchKernelGGL((k_dense_prepare<TI, TO>), dim3(n), dim3(256), 0, st, a, r);
   const bool padded = p.cut && p.dz;  // whether the rows of both operands go on, as zeros, to a multiple of 32
   Product dx{}, dw{};
