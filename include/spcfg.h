@@ -309,7 +309,11 @@ int spcfg_distill_workspace_bytes(int32_t rows, int32_t V, size_t* out_bytes);
 int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,
                           const int32_t* teacher_ids, float temperature, float* loss, float* lse, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
-/* The gradient alone, from the lse that a forward call on the same inputs wrote. */
+/*
+ * The gradient alone, from the lse that a forward call on the same inputs wrote.  Rows that a workgroup can hold (see below) take their
+ * sums again: the result is that of the joint call, bit for bit.  Longer rows go by lse: its rounding to 32 bits, up to 2^-24 |lse|,
+ * is a relative error of q, the same all along the row, and an lse that is not finite (beyond 3.4e38) makes the row's gradient NaN.
+ */
 int spcfg_distill_backward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,
                            const int32_t* teacher_ids, float temperature, const float* lse, const float* grad_loss,
                            void* grad_logits, void* hip_stream);

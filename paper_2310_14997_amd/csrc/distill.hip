@@ -16,6 +16,7 @@
 namespace spcfg {
 namespace {
 
+constexpr double kLog2e = 1.4426950408889634;
 constexpr int kMostEntries = 1024;  // of the teacher's, a row: they are kept in LDS, 10 bytes each
 
 typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
@@ -298,6 +299,8 @@ __device__ __forceinline__ float row_scale(const Args& g, float weight, bool som
 }
 
 // ---- a row per workgroup, in registers ----------------------------------------------------------------------------------
+// The gradient alone (no place for the loss) takes the row's sum again: an lse in 32 bits is good to 2^-24 of itself only, and q would
+// be off by that much times |lse| (2.4e-5 at 400, scores of +-4 at a temperature of 0.01), all of a row to the same side.
 template <typename T, int NT, int E, bool GRAD>
 __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   constexpr int W = Row<T>::W;
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
     const float scale = row_scale(g, weight, tr.some, tr.bad);
     write<T, NT, E>(g, ent, s, row, 0, nv, head, x, scale, inv, [&](int e) { return ent.w[e] * tr.inv; });
   }
-  if (threadIdx.x < 64) {
+  if (threadIdx.x < 64 && (!GRAD || g.loss)) {
     double terms, sum;
     loss_terms<T>(g, row, ent, tr, &terms, &sum);
     if (threadIdx.x == 0) {
@@ -406,10 +409,11 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_stats(Args g) {
 }
 
 // JOIN: from the parts' maxima and sums and the row's record, part 0 writing loss and lse; otherwise from the lse that the caller
-// kept
-template <typename T, int NT, int E, bool JOIN, bool GRAD>
-__global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
-  constexpr int W = Row<T>::W;
+// kept, with the exponents s / tau - lse in 64 bits, so that the rounding of lse is all that q loses.  Where lse is not finite (it
+// may not fit 32 bits at a tiny temperature) the gradient is NaN.
+template <typename T, int E, bool JOIN, bool GRAD>
+__global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int parts_here) {
+  constexpr int W = Row<T>::W, NT = kPartThreads;
   __shared__ float red[96];
   extern __shared__ __attribute__((aligned(16))) int lds[];
   Entries ent(lds, g.k);
@@ -430,6 +434,7 @@ __global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
   if constexpr (GRAD) empty<T, NT>(head);
   Teacher tr;
   float m, inv;
+  double by_two = 0.0, from = 0.0;
   if (JOIN) {
     // (every wavefront joins the parts for itself: no barrier to wait at)
     const RowTeacher rec = g.rec[row];
@@ -457,19 +462,19 @@ __global__ void __launch_bounds__(NT) k_distill_finish(Args g, int parts_here) {
       g.lse[row] = (float)lse;
     }
   } else {
-    tr = teacher_row<T, NT>(g, row, ent, red, [&] {
-      if (NT == 64) __syncthreads();
-      hang<T, NT>(g, ent, s, first, last, head);
-    });
-    if (NT == 64) __syncthreads();
-    m = g.lse_in[row] * g.tau;  // exp((s - tau lse) / tau) is q itself
-    inv = 1.0f;
+    tr = teacher_row<T, NT>(g, row, ent, red, [&] { hang<T, NT>(g, ent, s, first, last, head); });
+    const float lse = g.lse_in[row];
+    m = 0.0f;
+    inv = fabsf(lse) < INFINITY ? 1.0f : NAN;
+    by_two = kLog2e / g.tau;
+    from = lse * kLog2e;
   }
   if constexpr (GRAD) {
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int u = 0; u < W; ++u) x[e][u] = power(g, x[e][u] - m);
+      for (int u = 0; u < W; ++u)
+        x[e][u] = JOIN ? power(g, x[e][u] - m) : __builtin_amdgcn_exp2f((float)(x[e][u] * by_two - from));
     write<T, NT, E>(g, ent, s, row, first, last, head, x, row_scale(g, weight, tr.some, tr.bad), inv,
                     [&](int e) { return (JOIN ? power(g, ent.w[e] - tr.top) : ent.w[e]) * tr.inv; });
   }
@@ -508,22 +513,25 @@ void each(int n, F launch) {
   else launch(std::integral_constant<int, kMostEach>());
 }
 
+// rows that a workgroup holds
+template <typename T, bool GRAD>
+void launch_rows(const Args& a, hipStream_t st) {
+  const int64_t nv = row_vectors(a.V, Row<T>::W);
+  const unsigned lds = entries_bytes(a.k);
+  const dim3 grid((unsigned)a.R);
+  if (nv <= 64 * 2) hipLaunchKernelGGL((k_distill_rows<T, 64, 2, GRAD>), grid, dim3(64), lds, st, a);
+  else if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), lds, st, a);
+  else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), lds, st, a);
+  else if (a.R <= kFewRows && nv <= 512 * 3) hipLaunchKernelGGL((k_distill_rows<T, 512, 3, GRAD>), grid, dim3(512), lds, st, a);
+  else if (nv <= 256 * 6) hipLaunchKernelGGL((k_distill_rows<T, 256, 6, GRAD>), grid, dim3(256), lds, st, a);
+  else if (nv <= 512 * 5) hipLaunchKernelGGL((k_distill_rows<T, 512, 5, GRAD>), grid, dim3(512), lds, st, a);
+  else hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), lds, st, a);
+}
 template <typename T, bool GRAD>
 void launch_forward(Args a, hipStream_t st) {
   constexpr int W = Row<T>::W;
-  const int64_t nv = row_vectors(a.V, W);
+  if (in_registers(a.V, W)) return launch_rows<T, GRAD>(a, st);
   const unsigned lds = entries_bytes(a.k);
-  if (in_registers(a.V, W)) {
-    const dim3 grid((unsigned)a.R);
-    if (nv <= 64 * 2) hipLaunchKernelGGL((k_distill_rows<T, 64, 2, GRAD>), grid, dim3(64), lds, st, a);
-    else if (nv <= 64 * 4) hipLaunchKernelGGL((k_distill_rows<T, 64, 4, GRAD>), grid, dim3(64), lds, st, a);
-    else if (nv <= 256 * 4) hipLaunchKernelGGL((k_distill_rows<T, 256, 4, GRAD>), grid, dim3(256), lds, st, a);
-    else if (a.R <= kFewRows && nv <= 512 * 3) hipLaunchKernelGGL((k_distill_rows<T, 512, 3, GRAD>), grid, dim3(512), lds, st, a);
-    else if (nv <= 256 * 6) hipLaunchKernelGGL((k_distill_rows<T, 256, 6, GRAD>), grid, dim3(256), lds, st, a);
-    else if (nv <= 512 * 5) hipLaunchKernelGGL((k_distill_rows<T, 512, 5, GRAD>), grid, dim3(512), lds, st, a);
-    else hipLaunchKernelGGL((k_distill_rows<T, 512, 8, GRAD>), grid, dim3(512), lds, st, a);
-    return;
-  }
   const Split sp = split_of(a.R, a.V, W);
   a.parts = sp.parts;
   a.span = sp.span;
@@ -531,27 +539,19 @@ void launch_forward(Args a, hipStream_t st) {
   each(sp.each, [&](auto e) {
     constexpr int E = decltype(e)::value;
     hipLaunchKernelGGL((k_distill_stats<T, E>), dim3((unsigned)(a.R * (sp.parts + 1))), dim3(kPartThreads), lds, st, a);
-    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)),
-                       dim3(kPartThreads), lds, st, a, here);
+    hipLaunchKernelGGL((k_distill_finish<T, GRAD ? E : 1, true, GRAD>), dim3((unsigned)(a.R * here)), dim3(kPartThreads), lds, st, a,
+                       here);
   });
 }
 template <typename T>
 void launch_backward(Args a, hipStream_t st) {
-  const int64_t nv = row_vectors(a.V, Row<T>::W);
-  const unsigned lds = entries_bytes(a.k);
-  // many short rows: 8192 rows of 300 floats 11.1 us, 16.2 with 256 threads a row; 60 rows 4.7 and 4.4 us
-  if (nv <= 64 * 2 && a.R > kFewRows) {
-    a.parts = 1;
-    a.span = nv;
-    hipLaunchKernelGGL((k_distill_finish<T, 64, 2, false, true>), dim3((unsigned)a.R), dim3(64), lds, st, a, 1);
-    return;
-  }
+  if (in_registers(a.V, Row<T>::W)) return launch_rows<T, true>(a, st);
   const Split sp = split_of(a.R, a.V, Row<T>::W);
   a.parts = sp.parts;
   a.span = sp.span;
   each(sp.each, [&](auto e) {
-    hipLaunchKernelGGL((k_distill_finish<T, kPartThreads, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)),
-                       dim3(kPartThreads), lds, st, a, sp.parts);
+    hipLaunchKernelGGL((k_distill_finish<T, decltype(e)::value, false, true>), dim3((unsigned)(a.R * sp.parts)), dim3(kPartThreads),
+                       entries_bytes(a.k), st, a, sp.parts);
   });
 }
 
@@ -581,7 +581,7 @@ int check(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, 
   const int rc = check_sizes(rows, V);
   if (rc) return rc;
   if (k < 1 || k > kMostEntries) return SPCFG_ERR_SHAPE;
-  const double by_two = 1.4426950408889634 / tau;
+  const double by_two = kLog2e / tau;
   if (!(tau > 0.0f) || !(tau < INFINITY) || !((float)by_two < INFINITY)) return SPCFG_ERR_ARG;
   if (rows > 0 && (!logits || !teacher || !ids)) return SPCFG_ERR_ARG;
   const uintptr_t mask = type == SPCFG_TYPE_F32 ? 3 : 1;

@@ -1,0 +1,82 @@
+"""GPU tests of distillation where it is easily wrong: low temperatures, whose lse is large.
+
+Tolerances with u = 2^-24 as in test_gpu_distill.py, but for the gradient alone: the joint call's, bit for bit, where a workgroup holds a
+row; of longer rows, the joint call's and u |lse| of q, the rounding of the kept lse (exponents are formed in 64 bits)."""
+import numpy as np
+import pytest
+
+from oracle import losses_oracle as LO
+from operator_util import close, put, values
+from paper_2310_14997_amd import binding as bd
+from test_gpu_distill import dtype, inputs, scratch
+
+pytestmark = pytest.mark.gpu
+
+
+def calls(s, t, ids, tau, g, bf16):
+    """gradient of the joint call, gradient alone, lse"""
+    import torch
+    (R, V), f = s.shape, torch.float32
+    ts, tt, ti = put(s, dtype(bf16)), put(t, dtype(bf16)), put(ids, torch.int32)
+    tw = None if g is None else put(g, f)
+    e = lambda *n, d=f: torch.full(n, float("nan"), dtype=d, device="cuda:0")
+    loss, lse, both, alone = e(R), e(R), e(R, V, d=dtype(bf16)), e(R, V, d=dtype(bf16))
+    bd.spcfg_distill_forward_backward(ts, tt, ti, tau, tw, loss, lse, both, scratch(R, V))
+    bd.spcfg_distill_backward(ts, tt, ti, tau, lse, tw, alone)
+    return both, alone, lse
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [300, 900, 5000, 16000, 40000])
+@pytest.mark.parametrize("tau,by", [(0.01, 1.0), (0.01, 14.0), (1.0, 300.0)])
+def test_gradients_alone_at_low_temperatures(V, bf16, tau, by):
+    """|lse| up to some thousands; in fp32 the rows' q add up to 1 within the tolerance too, which an error of one sign would break."""
+    import torch
+    R, k = 6, 8
+    print("case distill low temperature", V, bf16, tau, by, flush=True)
+    s, t, ids, g = inputs(R, V, k, bf16, seed=8)
+    s, t = (np.clip(by * x, -5 * by, 5 * by) for x in (s, t))
+    if bf16:
+        s, t = (torch.from_numpy(x).to(torch.bfloat16).double().numpy() for x in (s, t))
+    s[0], s[1] = np.float32(4.7 * by) if not bf16 else 4.0 * by, s[1] / 64  # a row of equal scores, a row of scores close together
+    s, t = (torch.from_numpy(x).to(dtype(bf16)).double().numpy() for x in (s, t))  # the values that the call sees
+    both, alone, lse = calls(s, t, ids, tau, g, bf16)
+    if V <= 16000:
+        assert torch.equal(both, alone)
+    _, want_lse, grad = LO.distill(s, t, ids, tau, g)
+    q = np.exp(s / tau - want_lse[:, None])
+    p = q - grad / np.where(g == 0, 1.0, g)[:, None] / tau
+    tg = np.abs(g)[:, None] * tau * (2.0 ** -18 * q + 2.0 ** -20 * np.abs(p)) + (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(grad) \
+        + 2.0 ** -126 * (1 + np.abs(g)[:, None] * tau)
+    # exponents, (s - max) / tau of q and (t - max) / tau = log p + log sum of p, the sum at most k, are rounded at 2^-24 of themselves
+    # three times: at a low temperature that is more than the 2^-18 and 2^-20 above
+    x_p = np.where(np.abs(p) > 1e-300, np.log(k) - np.log(np.maximum(np.abs(p), 1e-300)), 0.0)
+    tg = tg + np.abs(g)[:, None] * tau * 3 * 2.0 ** -24 * (q * (s.max(1, keepdims=True) - s) / tau + np.abs(p) * x_p)
+    close("both", values(both), grad, tg)
+    kept = 2.0 ** -24 * np.abs(want_lse)[:, None] * (V > 16000)
+    close("alone", values(alone), grad, tg + np.abs(g)[:, None] * tau * q * kept)
+    if not bf16:
+        rows = (ids >= 0).any(axis=1) & (g != 0)
+        off = np.abs(values(alone)[rows].sum(1)) / (tau * g[rows])
+        assert np.all(off <= 2.0 ** -17 + kept[rows, 0]), (off, kept[rows, 0])
+
+
+@pytest.mark.parametrize("V", [40, 6000, 50000])
+def test_temperatures_whose_lse_does_not_fit(V):
+    """lse is 5 / 1e-38: the gradient is that of the joint call where a workgroup holds the row, and NaN, not zeros, where it does not."""
+    import torch
+    rng = np.random.default_rng(3)
+    s = rng.integers(-5, 5, size=(3, V)).astype(np.float64)
+    s[:, 7] = 5.0
+    t, ids = np.zeros((3, 2)), np.array([[7, 9], [11, -1], [-1, -1]], np.int32)
+    g = np.full(3, 2.0 ** 120)
+    both, alone, lse = calls(s, t, ids, 1e-38, g, False)
+    assert bool(torch.isinf(lse).all())
+    by = 2.0 ** 120 * np.float32(1e-38)
+    want = np.zeros((3, V))
+    want[0, 7], want[0, 9], want[1, 7], want[1, 11] = 0.5 * by, -0.5 * by, by, -by
+    close("both", values(both), want, 2.0 ** -22 * np.abs(want))
+    if V <= 16000:
+        assert torch.equal(both, alone)
+    else:
+        assert bool(torch.isnan(alone[:2]).all()) and not bool(alone[2].any())
