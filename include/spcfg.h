@@ -300,8 +300,8 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
  *                  overlaps nothing else
  *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted); holds
  *                  nothing between calls, calls that may overlap need their own
- * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An id >= V gives the row's loss and
- * gradient NaN, and so does a NaN among its scores; a student's score of -inf where p > 0 gives an infinite loss and a
+ * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An entry that is there with an id >= V
+ * gives the row's loss and gradient NaN, and so does a NaN among its scores; a student's score of -inf where p > 0 gives an infinite loss and a
  * finite gradient.  Matrices are dense, pointers need the alignment of one element.  rows may be 0; rows <= 2^20,
  * V <= 2^24, rows * V <= 2^36.  Deterministic.
  */

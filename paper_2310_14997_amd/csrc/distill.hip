@@ -142,7 +142,7 @@ struct Teacher {
   bool some, bad;       // whether any entry is there; whether an id is out of range or a score NaN or +inf
 };
 
-// Fills E with the row's ids and scores; an entry with a negative id or a score of -inf is absent.  This thread's share of the
+// Fills E with the row's ids and scores; an entry with a negative id or a score of -inf is absent, whatever else it holds.  This thread's share of the
 // largest score, and of whether something is wrong.
 template <typename T, int NT>
 __device__ __forceinline__ void load_entries(const Args& g, int64_t row, Entries& E, float* top, float* wrong) {
@@ -153,7 +153,7 @@ __device__ __forceinline__ void load_entries(const Args& g, int64_t row, Entries
   for (int e = threadIdx.x; e < g.k; e += NT) {
     int id = ids[e];
     const float a = to_float<T>(t[e]);
-    if (id >= 0 && (id >= g.V || !(a < INFINITY))) *wrong = 1.0f;
+    if (id >= 0 && a != -INFINITY && (id >= g.V || !(a < INFINITY))) *wrong = 1.0f;
     if (id >= g.V || a == -INFINITY) id = -1;
     E.id[e] = id < 0 ? -1 : id;
     E.w[e] = a;

@@ -80,3 +80,26 @@ def test_temperatures_whose_lse_does_not_fit(V):
         assert torch.equal(both, alone)
     else:
         assert bool(torch.isnan(alone[:2]).all()) and not bool(alone[2].any())
+
+
+@pytest.mark.parametrize("V", [40, 6000, 50000])
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_padding_by_scores_of_minus_infinity(V, bf16):
+    """Entries that pad a row, with a score of -inf and any id, one past the last among them, are absent: as with an id of -1."""
+    import torch
+    R, k, f = 4, 6, torch.float32
+    s, t, ids, g = inputs(R, V, k, bf16, seed=2, absent=0.0)
+    ids[0, 2:], ids[1, 5], ids[2] = -1, -1, -1
+    ids[3] = [1, 0, 9, 5, 7, 3]
+    padded, scores = ids.copy(), t.copy()
+    padded[0, 2:], padded[1, 5], padded[2] = V, 2 ** 31 - 1, [V, V + 1, 0, 3, V, -5]
+    scores[ids < 0] = -np.inf
+    one, _, lse_one = calls(s, t, ids, 2.0, g, bf16)
+    two, alone, lse_two = calls(s, scores, padded, 2.0, g, bf16)
+    assert bool(torch.isfinite(one).all()) and torch.equal(one, two) and torch.equal(lse_one, lse_two)
+    assert bool(torch.isfinite(alone).all()) and not bool(two[2].any())
+    out = [torch.empty(R, device="cuda:0") for _ in range(4)]
+    ts = put(s, dtype(bf16))
+    bd.spcfg_distill_forward(ts, put(t, dtype(bf16)), put(ids, torch.int32), 2.0, out[0], out[1], scratch(R, V))
+    bd.spcfg_distill_forward(ts, put(scores, dtype(bf16)), put(padded, torch.int32), 2.0, out[2], out[3], scratch(R, V))
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3]) and float(out[0][2]) == 0.0
