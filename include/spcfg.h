@@ -301,9 +301,9 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
  *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted); holds
  *                  nothing between calls, calls that may overlap need their own
  * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An entry that is there with an id >= V
- * gives the row's loss and gradient NaN, and so does a NaN among its scores; a student's score of -inf where p > 0 gives an infinite loss and a
- * finite gradient.  Matrices are dense, pointers need the alignment of one element.  rows may be 0; rows <= 2^20,
- * V <= 2^24, rows * V <= 2^36.  Deterministic.
+ * gives the row's loss and gradient NaN, and so does a NaN among its scores; a row of nothing but -inf has lse -inf and, with entries,
+ * loss and gradient NaN; a student's score of -inf where p > 0 gives an infinite loss and a finite gradient.  Matrices are dense,
+ * pointers need the alignment of one element.  rows may be 0; rows <= 2^20, V <= 2^24, rows * V <= 2^36.  Deterministic.
  */
 int spcfg_distill_workspace_bytes(int32_t rows, int32_t V, size_t* out_bytes);
 int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,

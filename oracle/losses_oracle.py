@@ -2,7 +2,7 @@
 
 Distillation, row by row: p = softmax(teacher / tau) over the entries that are there (id >= 0, score above -inf),
 q = softmax(logits / tau): loss = tau^2 sum_e p_e (log p_e - log q_id(e)), gradient tau (q - p at its ids); a row
-without entries is 0 and 0.
+without entries is 0 and 0, and one of nothing but -inf has lse -inf and, with entries, NaN.
 
 Preference: margin = (logZ_c - ref_c) - (logZ_r - ref_r), x = beta margin, loss = (1 - eps) log(1 + exp(-x)) +
 eps log(1 + exp(x)), gradient in logZ; absent pairs (a negative index) are 0.
@@ -22,6 +22,11 @@ def distill(logits, teacher, ids, tau, grad_loss=None):
     loss, lse, grad = np.zeros(R), np.zeros(R), np.zeros((R, V))
     for r in range(R):
         m = s[r].max()
+        if m == -np.inf:  # nothing that the row could be
+            lse[r], loss[r], grad[r] = m, np.nan, np.nan
+            if not any(ids[r][e] >= 0 and teacher[r][e] > -np.inf for e in range(len(ids[r]))):
+                loss[r], grad[r] = 0.0, 0.0
+            continue
         lse[r] = m + np.log(np.exp(s[r] - m).sum())
         there = [e for e in range(len(ids[r])) if ids[r][e] >= 0 and teacher[r][e] > -np.inf]
         if not there:

@@ -54,6 +54,10 @@ struct RowTeacher {
 // 0.  (With expf, which splits its argument, 4096 rows of 8000 bf16 scores take 38.8 us instead of 34.0.)
 __device__ __forceinline__ float power(const Args& g, float d) { return __builtin_amdgcn_exp2f(d * g.by_two); }
 
+// What a row's scores are taken from: their maximum, where that is -inf 0.  The sum is 0 then, lse = -inf, and loss and gradient are
+// NaN, as 0 / 0 has it.
+__device__ __forceinline__ float from_top(float m) { return m == -INFINITY ? 0.0f : m; }
+
 // ---- sums and maxima over a workgroup of NT threads, N values at a time, in a fixed order --------------------------------
 // (one barrier: a kernel gives each call 48 floats of its own)
 template <typename F, typename X> __device__ __forceinline__ X across_wave(X v, F f) {
@@ -329,14 +333,13 @@ __global__ void __launch_bounds__(NT) k_distill_rows(Args g) {
   all<NT, 3>(v, red, Max());  // (behind it every entry's id is in LDS)
   if (NT == 64) __syncthreads();
   if constexpr (GRAD) hang<T, NT>(g, ent, s, 0, nv, head);
-  const float m = v[0];
+  const float m = from_top(v[0]);
   float sums[2] = {0.0f, weigh_entries<NT>(g, ent, v[1])};
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (e * NT < nv) {
 #pragma unroll
       for (int u = 0; u < W; ++u) {
-        // outside the row -inf gives 0, unless the whole row is -inf: NaN, as the definition has it
         x[e][u] = power(g, x[e][u] - m);
         sums[0] += x[e][u];
       }
@@ -448,11 +451,11 @@ __global__ void __launch_bounds__(kPartThreads) k_distill_finish(Args g, int par
     }
     m = -INFINITY;
     for (int c = lane; c < g.parts; c += 64) m = fmaxf(m, g.stat[row * g.parts + c].x);
-    m = across_wave(m, Max());
+    m = from_top(across_wave(m, Max()));
     float sum = 0.0f;
     for (int c = lane; c < g.parts; c += 64) {
       const float2 v = g.stat[row * g.parts + c];
-      sum += v.y * power(g, v.x - m);  // a part of nothing but -inf adds 0, a row of nothing else gives NaN
+      sum += v.y * power(g, v.x - m);  // (a part of nothing but -inf adds 0)
     }
     sum = across_wave(sum, Add());
     inv = 1.0f / sum;

@@ -103,3 +103,29 @@ def test_padding_by_scores_of_minus_infinity(V, bf16):
     bd.spcfg_distill_forward(ts, put(t, dtype(bf16)), put(ids, torch.int32), 2.0, out[0], out[1], scratch(R, V))
     bd.spcfg_distill_forward(ts, put(scores, dtype(bf16)), put(padded, torch.int32), 2.0, out[2], out[3], scratch(R, V))
     assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3]) and float(out[0][2]) == 0.0
+
+
+@pytest.mark.parametrize("V", [40, 1000, 6000, 50000])
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_rows_of_nothing_but_minus_infinity(V, bf16):
+    """lse is the log of an empty sum; loss and gradient are NaN with entries and 0 without; a NaN in the row, or one finite score, counts."""
+    import torch
+    inf = np.inf
+    s = np.full((5, V), -inf)
+    s[2, V - 3], s[3, V // 2] = np.nan, -3.0
+    s[4] = 0.0
+    t, ids = np.zeros((5, 2)), np.tile(np.array([[1, 2]], np.int32), (5, 1))
+    ids[1] = -1
+    both, alone, lse = calls(s, t, ids, 2.0, None, bf16)
+    loss, lse_alone = torch.empty(5, device="cuda:0"), torch.empty(5, device="cuda:0")
+    bd.spcfg_distill_forward(put(s, dtype(bf16)), put(t, dtype(bf16)), put(ids, torch.int32), 2.0, loss, lse_alone, scratch(5, V))
+    want_loss, want_lse, want = LO.distill(s[[0, 1, 3]], t[[0, 1, 3]], ids[[0, 1, 3]], 2.0)
+    assert want_lse[0] == -inf and want_lse[1] == -inf and np.isnan(want_loss[0]) and want_loss[1] == 0 and want_loss[2] == inf
+    for got in (values(lse), values(lse_alone)):
+        assert got[0] == -inf and got[1] == -inf and np.isnan(got[2]) and got[3] == -1.5 and abs(got[4] - np.log(V)) < 2.0 ** -18
+    got = values(loss)
+    assert np.isnan(got[0]) and got[1] == 0 and np.isnan(got[2]) and got[3] == inf
+    for g in (values(both), values(alone)):
+        assert np.isnan(g[0]).all() and np.isnan(want[0]).all() and not g[1].any() and np.isnan(g[2]).all()
+        step = 2.0 ** -8 if bf16 else 2.0 ** -24
+        assert np.all(np.abs(g[3] - want[2]) <= step * np.abs(want[2]) + 2.0 ** -19 * 2)
