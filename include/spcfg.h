@@ -266,7 +266,7 @@ int spcfg_dense_workspace_bytes(const spcfg_dense_config* cfg, size_t* out_bytes
  *   preact     dev [rows x out] or NULL: z, for the backward pass (only needed with an activation)
  *   workspace  dev, 256-byte aligned, >= spcfg_dense_workspace_bytes(...) bytes; holds nothing between calls.  Calls and
  *              replays of captured ones that may overlap need workspaces of their own
- * residual may be x (where the types and sizes allow it) and y may be residual; outputs overlap nothing else.
+ * residual may be x (where the types and sizes allow it) and y may be residual; outputs and workspace overlap nothing else.
  */
 int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void* W, const void* bias, const void* residual,
                         void* y, void* preact, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -279,7 +279,7 @@ int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void
  *   preact      dev [rows x out]: z as the forward call wrote it; NULL with SPCFG_ACT_NONE
  *   grad_x_add  dev [rows x in] or NULL: added to grad_x.  A layer whose residual is x itself passes grad_y here
  * SPCFG_FLAG_ACCUMULATE_GRADS adds to grad_W and grad_bias (in their type).  grad_x may be grad_x_add (unless that is
- * grad_y); outputs overlap nothing else.  Sums run in a fixed order: results are deterministic.
+ * grad_y); outputs and workspace overlap nothing else.  Sums run in a fixed order: results are deterministic.
  */
 int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const void* W, const void* preact, const void* grad_y,
                          const void* grad_x_add, void* grad_x, void* grad_W, void* grad_bias, void* workspace,
@@ -296,14 +296,14 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
  *   temperature    > 0, finite, and so is 1.5 / temperature
  *   loss, lse      dev [rows] float: out
  *   grad_loss      dev [rows] float or NULL (= all ones): what each row's loss counts in the sum that is differentiated
- *   grad_logits    dev [rows x V] of `type`: grad_loss * temperature * (q_j - sum of the p_e with id(e) = j); overwritten,
- *                  overlaps nothing else
+ *   grad_logits    dev [rows x V] of `type`: grad_loss * temperature * (q_j - sum of the p_e with id(e) = j); overwritten
  *   workspace      dev, 256-byte aligned, >= spcfg_distill_workspace_bytes(rows, V) (may be 0: then NULL is accepted); holds
  *                  nothing between calls, calls that may overlap need their own
  * A row without entries has loss 0 and gradient 0, a row with grad_loss 0 has gradient 0.  An entry that is there with an id >= V
  * gives the row's loss and gradient NaN, and so does a NaN among its scores; a row of nothing but -inf has lse -inf and, with entries,
  * loss and gradient NaN; a student's score of -inf where p > 0 gives an infinite loss and a finite gradient.  Matrices are dense,
- * pointers need the alignment of one element.  rows may be 0; rows <= 2^20, V <= 2^24, rows * V <= 2^36.  Deterministic.
+ * pointers need the alignment of one element; outputs and workspace overlap nothing else.  rows may be 0; rows <= 2^20, V <= 2^24,
+ * rows * V <= 2^36.  Deterministic.
  */
 int spcfg_distill_workspace_bytes(int32_t rows, int32_t V, size_t* out_bytes);
 int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher_logits,

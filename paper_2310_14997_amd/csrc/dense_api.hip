@@ -24,8 +24,7 @@ size_t need(const spcfg_dense_config* c) {
   return c->rows == 0 ? 0 : dense::tiled_workspace(c->rows, c->in, c->out, c->in_type, c->out_type, c->activation);
 }
 
-int check_workspace(const spcfg_dense_config* c, const void* ws, size_t bytes) {
-  const size_t n = need(c);
+int check_workspace(size_t n, const void* ws, size_t bytes) {
   if (n == 0) return SPCFG_OK;
   if (!ws) return SPCFG_ERR_ARG;
   return ((uintptr_t)ws & 255) != 0 || bytes < n ? SPCFG_ERR_WORKSPACE : SPCFG_OK;
@@ -33,13 +32,7 @@ int check_workspace(const spcfg_dense_config* c, const void* ws, size_t bytes) {
 
 bool on_type(const void* p, int type) { return ((uintptr_t)p & (type == SPCFG_TYPE_F32 ? 3 : 1)) == 0; }
 
-// whether [p, p + n elements) and [q, q + m elements) share memory; nothing does with an absent one
-bool overlap(const void* p, int64_t n, int tp, const void* q, int64_t m, int tq) {
-  if (!p || !q || n == 0 || m == 0) return false;
-  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  const uintptr_t ea = a + (uintptr_t)n * (tp == SPCFG_TYPE_F32 ? 4 : 2), eb = b + (uintptr_t)m * (tq == SPCFG_TYPE_F32 ? 4 : 2);
-  return a < eb && b < ea;
-}
+int64_t size_of(int type) { return type == SPCFG_TYPE_F32 ? 4 : 2; }
 
 dense::Args args_of(const spcfg_dense_config* c) {
   dense::Args a{};
@@ -73,14 +66,11 @@ int spcfg_dense_forward(const spcfg_dense_config* cfg, const void* x, const void
   if (!on_type(x, ti) || !on_type(W, ti) || !on_type(bias, ti) || !on_type(residual, to) || !on_type(y, to) || !on_type(preact, to))
     return SPCFG_ERR_ARG;
   dense::Args a = args_of(cfg);
-  const int64_t nx = a.R * a.I, nw = a.O * a.I, ny = a.R * a.O;
-  const void* outs[2] = {y, preact};
-  for (const void* o : outs) {
-    if (overlap(o, ny, to, x, nx, ti) || overlap(o, ny, to, W, nw, ti) || overlap(o, ny, to, bias, a.O, ti)) return SPCFG_ERR_ARG;
-    if (!(o == y && y == residual) && overlap(o, ny, to, residual, ny, to)) return SPCFG_ERR_ARG;
-  }
-  if (overlap(y, ny, to, preact, ny, to)) return SPCFG_ERR_ARG;
-  if ((rc = check_workspace(cfg, workspace, workspace_bytes))) return rc;
+  const int64_t si = size_of(ti), nx = a.R * a.I * si, nw = a.O * a.I * si, ny = a.R * a.O * size_of(to);
+  const size_t n = need(cfg);
+  const Memory all[] = {{y, ny}, {preact, ny}, {workspace, (int64_t)n}, {x, nx}, {W, nw}, {bias, a.O * si}, {residual, ny}};
+  if (clash(all, 3, 7, 0, 6)) return SPCFG_ERR_ARG;
+  if ((rc = check_workspace(n, workspace, workspace_bytes))) return rc;
   a.x = x; a.W = W; a.bias = bias; a.residual = residual; a.y = y; a.preact = preact;
   if (!dense::tiled_forward(a, ti, to, workspace, (hipStream_t)hip_stream))
     dense::launch_direct_forward(a, ti, to, (hipStream_t)hip_stream);
@@ -101,18 +91,12 @@ int spcfg_dense_backward(const spcfg_dense_config* cfg, const void* x, const voi
       !on_type(grad_x, ti) || !on_type(grad_W, ti) || !on_type(grad_bias, ti))
     return SPCFG_ERR_ARG;
   dense::Args a = args_of(cfg);
-  const int64_t nx = a.R * a.I, nw = a.O * a.I, ny = a.R * a.O;
-  const void* out[3] = {grad_x, grad_W, grad_bias};
-  const int64_t len[3] = {nx, nw, a.O};
-  for (int i = 0; i < 3; ++i) {
-    if (overlap(out[i], len[i], ti, x, nx, ti) || overlap(out[i], len[i], ti, W, nw, ti) ||
-        overlap(out[i], len[i], ti, preact, ny, to) || overlap(out[i], len[i], ti, grad_y, ny, to))
-      return SPCFG_ERR_ARG;
-    if (!(i == 0 && grad_x == grad_x_add) && overlap(out[i], len[i], ti, grad_x_add, nx, ti)) return SPCFG_ERR_ARG;
-    for (int j = 0; j < i; ++j)
-      if (overlap(out[i], len[i], ti, out[j], len[j], ti)) return SPCFG_ERR_ARG;
-  }
-  if ((rc = check_workspace(cfg, workspace, workspace_bytes))) return rc;
+  const int64_t si = size_of(ti), nx = a.R * a.I * si, nw = a.O * a.I * si, ny = a.R * a.O * size_of(to);
+  const size_t n = need(cfg);
+  const Memory all[] = {{grad_x, nx}, {grad_W, nw}, {grad_bias, a.O * si}, {workspace, (int64_t)n}, {x, nx}, {W, nw}, {preact, ny},
+                        {grad_y, ny}, {grad_x_add, nx}};
+  if (clash(all, 4, 9, 0, 8)) return SPCFG_ERR_ARG;
+  if ((rc = check_workspace(n, workspace, workspace_bytes))) return rc;
   if (cfg->rows == 0 && !grad_W) return SPCFG_OK;
   a.x = x; a.W = W; a.preact_in = act ? preact : nullptr; a.grad_y = grad_y; a.grad_x_add = grad_x_add;
   a.grad_x = cfg->rows > 0 ? grad_x : nullptr; a.grad_W = grad_W; a.grad_bias = grad_bias;

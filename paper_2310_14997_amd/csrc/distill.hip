@@ -572,11 +572,6 @@ int check_sizes(int32_t R, int32_t V) {
   return R < 0 || V < 1 || R > (1 << 20) || V > (1 << 24) || (int64_t)R * V > ((int64_t)1 << 36) ? SPCFG_ERR_SHAPE : SPCFG_OK;
 }
 
-bool overlap(const void* p, int64_t pb, const void* q, int64_t qb) {
-  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  return p && q && a < b + (uintptr_t)qb && b < a + (uintptr_t)pb;
-}
-
 // checks what all three calls share and fills their arguments
 int check(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, const void* teacher, const int32_t* ids,
           float tau, Args* a) {
@@ -594,14 +589,16 @@ int check(int32_t type, int32_t rows, int32_t V, int32_t k, const void* logits, 
   a->logits = logits; a->teacher = teacher; a->ids = ids;
   return SPCFG_OK;
 }
-int check_grad(int32_t type, const Args& a, const void* grad) {
+int check_grad(int32_t type, const Args& a) {
+  if (a.R > 0 && !a.grad) return SPCFG_ERR_ARG;
+  return ((uintptr_t)a.grad & (type == SPCFG_TYPE_F32 ? 3 : 1)) != 0 ? SPCFG_ERR_ARG : SPCFG_OK;
+}
+// outputs are written while other workgroups read: nothing shares their memory
+int check_memory(int32_t type, const Args& a, const void* ws) {
   const int64_t size = type == SPCFG_TYPE_F32 ? 4 : 2, n = a.R * a.V * size;
-  if (a.R > 0 && !grad) return SPCFG_ERR_ARG;
-  if ((uintptr_t)grad & (size - 1)) return SPCFG_ERR_ARG;
-  if (overlap(grad, n, a.logits, n) || overlap(grad, n, a.teacher, a.R * a.k * size) || overlap(grad, n, a.ids, a.R * a.k * 4) ||
-      overlap(grad, n, a.grad_loss, a.R * 4) || overlap(grad, n, a.lse_in, a.R * 4))
-    return SPCFG_ERR_ARG;
-  return SPCFG_OK;
+  const Memory all[] = {{a.loss, a.R * 4}, {a.lse, a.R * 4}, {a.grad, n}, {ws, ws ? (int64_t)need(a.R, a.V) : 0}, {a.logits, n},
+                        {a.teacher, a.R * a.k * size}, {a.ids, a.R * a.k * 4}, {a.grad_loss, a.R * 4}, {a.lse_in, a.R * 4}};
+  return clash(all, 4, 9) ? SPCFG_ERR_ARG : SPCFG_OK;
 }
 int check_workspace(int64_t R, int64_t V, const void* ws, size_t bytes) {
   const size_t n = need(R, V);
@@ -633,8 +630,10 @@ int spcfg_distill_forward(int32_t type, int32_t rows, int32_t V, int32_t k, cons
   if (rc) return rc;
   if (rows == 0) return SPCFG_OK;
   if (!loss || !lse) return SPCFG_ERR_ARG;
+  a.loss = loss; a.lse = lse;
+  if ((rc = check_memory(type, a, workspace))) return rc;
   if ((rc = check_workspace(rows, V, workspace, workspace_bytes))) return rc;
-  a.loss = loss; a.lse = lse; a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
+  a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
   if (type == SPCFG_TYPE_F32) launch_forward<float, false>(a, (hipStream_t)hip_stream);
   else launch_forward<uint16_t, false>(a, (hipStream_t)hip_stream);
   return launch_status();
@@ -649,7 +648,7 @@ int spcfg_distill_backward(int32_t type, int32_t rows, int32_t V, int32_t k, con
   if (rows == 0) return SPCFG_OK;
   if (!lse) return SPCFG_ERR_ARG;
   a.lse_in = lse; a.grad_loss = grad_loss; a.grad = grad_logits;
-  if ((rc = check_grad(type, a, grad_logits))) return rc;
+  if ((rc = check_grad(type, a)) || (rc = check_memory(type, a, nullptr))) return rc;
   if (type == SPCFG_TYPE_F32) launch_backward<float>(a, (hipStream_t)hip_stream);
   else launch_backward<uint16_t>(a, (hipStream_t)hip_stream);
   return launch_status();
@@ -664,10 +663,10 @@ int spcfg_distill_forward_backward(int32_t type, int32_t rows, int32_t V, int32_
   if (rc) return rc;
   if (rows == 0) return SPCFG_OK;
   if (!loss || !lse) return SPCFG_ERR_ARG;
-  a.grad_loss = grad_loss; a.grad = grad_logits;
-  if ((rc = check_grad(type, a, grad_logits))) return rc;
+  a.grad_loss = grad_loss; a.grad = grad_logits; a.loss = loss; a.lse = lse;
+  if ((rc = check_grad(type, a)) || (rc = check_memory(type, a, workspace))) return rc;
   if ((rc = check_workspace(rows, V, workspace, workspace_bytes))) return rc;
-  a.loss = loss; a.lse = lse; a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
+  a.rec = static_cast<RowTeacher*>(workspace); a.stat = reinterpret_cast<float2*>(a.rec + rows);
   if (type == SPCFG_TYPE_F32) launch_forward<float, true>(a, (hipStream_t)hip_stream);
   else launch_forward<uint16_t, true>(a, (hipStream_t)hip_stream);
   return launch_status();

@@ -118,14 +118,9 @@ int run(int32_t B, int32_t n, const float* logZ, const float* ref, const int32_t
   if (!logZ || (n > 0 && (!chosen || !rejected)) || (n > 0 && forward && (!loss || !margin)) || (backward && !grad))
     return SPCFG_ERR_ARG;
   // outputs are written while other workgroups read the inputs: none may share memory with anything else
-  const struct { const void* p; int64_t len; } at[] = {
-      {forward ? loss : nullptr, n}, {forward ? margin : nullptr, n}, {backward ? grad : nullptr, B},
-      {logZ, B}, {ref, B}, {chosen, n}, {rejected, n}, {grad_loss, n}};
-  for (int o = 0; o < 3; ++o)
-    for (int i = 0; i < 8; ++i) {
-      const uintptr_t a = (uintptr_t)at[o].p, b = (uintptr_t)at[i].p;
-      if (o != i && a && b && a < b + 4 * at[i].len && b < a + 4 * at[o].len) return SPCFG_ERR_ARG;
-    }
+  const Memory all[] = {{forward ? loss : nullptr, 4ll * n}, {forward ? margin : nullptr, 4ll * n}, {backward ? grad : nullptr, 4ll * B},
+                        {logZ, 4ll * B}, {ref, 4ll * B}, {chosen, 4ll * n}, {rejected, 4ll * n}, {grad_loss, 4ll * n}};
+  if (clash(all, 3, 8)) return SPCFG_ERR_ARG;
   const int pb = forward ? (n + 255) / 256 : 0, sb = backward ? (B + kOwn - 1) / kOwn : 0;
   if (pb + sb == 0) return SPCFG_OK;
   const Args a{B, n, logZ, ref, chosen, rejected, beta, eps, grad_loss, loss, margin, grad};

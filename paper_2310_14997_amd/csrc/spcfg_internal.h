@@ -45,6 +45,19 @@ constexpr int kExpZero = -(1 << 24);     // exponent marking an all-zero vector
 // Status of the launches of a call, for every entry point outside spcfg_api.hip too: keeps the runtime's message.
 int launch_status();
 
+// What a call reads or writes.  clash: whether one of the first `written` of n shares memory with any other; nothing does with an absent
+// or empty one, and `out` may be `in` itself (the same address) where these are given.
+struct Memory { const void* p; int64_t bytes; };
+inline bool clash(const Memory* m, int written, int n, int out = -1, int in = -1) {
+  for (int i = 0; i < written; ++i)
+    for (int j = 0; j < n; ++j) {
+      const uintptr_t a = (uintptr_t)m[i].p, b = (uintptr_t)m[j].p;
+      if (i == j || !a || !b || m[i].bytes <= 0 || m[j].bytes <= 0 || (a == b && ((i == out && j == in) || (i == in && j == out)))) continue;
+      if (a < b + (uintptr_t)m[j].bytes && b < a + (uintptr_t)m[i].bytes) return true;
+    }
+  return false;
+}
+
 constexpr int kMaxB = 960;               // lengths travel as one kernel argument
 constexpr int kMaxLen = 1024;
 
