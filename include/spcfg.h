@@ -336,8 +336,8 @@ int spcfg_distill_forward_backward(int32_t type, int32_t rows, int32_t V, int32_
  *   grad_logZ        dev [B]: gradient of sum_p grad_loss[p] * loss[p]; overwritten, 0 for sentences without pairs
  * A pair with a negative index is absent, and so is one whose margin is a difference of equal infinities (no grammar derives
  * either sentence): loss, margin and gradient 0.  An index >= B gives loss and margin NaN, and NaN as the gradient of the
- * pair's other sentence.  Outputs overlap nothing else.  1 <= B <= 65536, 0 <= pairs <= 2^20.  Deterministic; the gradient's cost
- * grows with B * pairs.
+ * pair's other sentence.  Pointers need the alignment of one element; outputs overlap nothing else.  1 <= B <= 65536,
+ * 0 <= pairs <= 2^20.  Deterministic; the gradient's cost grows with B * pairs.
  */
 int spcfg_preference_forward(int32_t B, int32_t pairs, const float* logZ, const float* ref_logZ, const int32_t* chosen,
                              const int32_t* rejected, float beta, float smoothing, float* loss, float* margin,

@@ -595,6 +595,8 @@ int check_grad(int32_t type, const Args& a) {
 }
 // outputs are written while other workgroups read: nothing shares their memory
 int check_memory(int32_t type, const Args& a, const void* ws) {
+  for (const float* p : {(const float*)a.loss, (const float*)a.lse, a.grad_loss, a.lse_in})
+    if ((uintptr_t)p & 3) return SPCFG_ERR_ARG;
   const int64_t size = type == SPCFG_TYPE_F32 ? 4 : 2, n = a.R * a.V * size;
   const Memory all[] = {{a.loss, a.R * 4}, {a.lse, a.R * 4}, {a.grad, n}, {ws, ws ? (int64_t)need(a.R, a.V) : 0}, {a.logits, n},
                         {a.teacher, a.R * a.k * size}, {a.ids, a.R * a.k * 4}, {a.grad_loss, a.R * 4}, {a.lse_in, a.R * 4}};

@@ -121,6 +121,8 @@ int run(int32_t B, int32_t n, const float* logZ, const float* ref, const int32_t
   const Memory all[] = {{forward ? loss : nullptr, 4ll * n}, {forward ? margin : nullptr, 4ll * n}, {backward ? grad : nullptr, 4ll * B},
                         {logZ, 4ll * B}, {ref, 4ll * B}, {chosen, 4ll * n}, {rejected, 4ll * n}, {grad_loss, 4ll * n}};
   if (clash(all, 3, 8)) return SPCFG_ERR_ARG;
+  for (const Memory& m : all)
+    if ((uintptr_t)m.p & 3) return SPCFG_ERR_ARG;
   const int pb = forward ? (n + 255) / 256 : 0, sb = backward ? (B + kOwn - 1) / kOwn : 0;
   if (pb + sb == 0) return SPCFG_OK;
   const Args a{B, n, logZ, ref, chosen, rejected, beta, eps, grad_loss, loss, margin, grad};
