@@ -304,7 +304,15 @@ def _scratch(t, dev):
     return t.data_ptr(), t.numel()
 
 
+def _fits(*sizes):
+    """Refuses sizes that the C interface's 32 bits would cut short."""
+    for n in sizes:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            _check(-2)
+
+
 def make_dense_config(rows, n_in, n_out, in_type=TYPE_F32, out_type=TYPE_F32, activation=ACT_NONE, flags=0):
+    _fits(rows, n_in, n_out)
     return DenseConfig(C.sizeof(DenseConfig), int(rows), int(n_in), int(n_out), int(in_type), int(out_type),
                        int(activation), int(flags))
 
@@ -347,6 +355,7 @@ def spcfg_dense_backward(cfg, x, W, preact, grad_y, grad_x_add, grad_x, grad_W, 
 
 
 def spcfg_distill_workspace_bytes(rows, V):
+    _fits(rows, V)
     out = C.c_size_t(0)
     _check(load().spcfg_distill_workspace_bytes(int(rows), int(V), C.byref(out)))
     return out.value
@@ -361,6 +370,7 @@ def _distill_inputs(logits, teacher_logits, teacher_ids, temperature):
     if not isinstance(teacher_ids, _torch.Tensor) or teacher_ids.dim() != 2:
         raise TypeError("teacher_ids must be a two-dimensional int32 device tensor")
     (rows, V), k = logits.shape, teacher_ids.shape[1]
+    _fits(rows, V, k)
     return dev, dtype, rows, V, (
         _FLOATS.index(dtype), rows, V, k, _here(logits, "logits", (rows, V), dtype, dev),
         _here(teacher_logits, "teacher_logits", (rows, k), dtype, dev),
@@ -401,6 +411,7 @@ def _preference_inputs(logZ, ref_logZ, chosen, rejected, beta, smoothing):
         if not isinstance(t, _torch.Tensor) or t.dim() != 1:
             raise TypeError(f"{name} must be a one-dimensional device tensor")
     (B,), (n,) = logZ.shape, chosen.shape
+    _fits(B, n)
     return dev, B, n, (
         B, n, _here(logZ, "logZ", (B,), _F32, dev), _here(ref_logZ, "ref_logZ", (B,), _F32, dev),
         _here(chosen, "chosen", (n,), _I32, dev), _here(rejected, "rejected", (n,), _I32, dev), float(beta), float(smoothing))
