@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(256) k_preference(Args g, int pair_blocks) {
       const int p = list[wave][h], c = g.chosen[p], r = g.rejected[p];
       bool out;
       const float m = margin_of(g, c, r, &out);
-      if (out || c == r) continue;  // (a sentence against itself adds and takes away the same)
+      if (out || (c == r && m == m)) continue;  // (a sentence against itself adds and takes away the same)
       const double w = (double)weight_of(g, m) * (g.grad_loss ? g.grad_loss[p] : 1.0f);
 #pragma unroll
       for (int u = 0; u < kOwn; ++u) {
