@@ -32,12 +32,12 @@ template <> struct Pieces<float> {
     s.cut(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]));
   }
   __device__ __forceinline__ void raw(const float (&v)[8]) { set(v); }
-  __device__ __forceinline__ void dz(const float (&v)[8], bool) { set(v); }
+  template <bool TWO> __device__ __forceinline__ void dz(const float (&v)[8]) { set(v); }
 };
 template <> struct Pieces<uint16_t> {
   Split2 s;
   __device__ __forceinline__ void raw(const uint16_t (&v)[8]) { __builtin_memcpy(&s.hi, v, 16); }
-  __device__ __forceinline__ void dz(const float (&v)[8], bool two) { s.cut(v, two); }
+  template <bool TWO> __device__ __forceinline__ void dz(const float (&v)[8]) { s.cut(v, TWO); }
 };
 
 // the matrix instruction of T x T: 16 k, resp. 32; lane l holds row l % T of an operand, k = 8 (l / T) .. + 7
@@ -58,8 +58,8 @@ template <> struct Mma<16> {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
-template <typename M>
-__device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<float>& b, bool, typename M::Acc& c) {
+template <typename M, bool TWO>
+__device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<float>& b, typename M::Acc& c) {
   c = M::mul(a.s.lo, b.s.hi, c);
   c = M::mul(a.s.hi, b.s.lo, c);
   c = M::mul(a.s.mid, b.s.mid, c);
@@ -67,9 +67,9 @@ __device__ __forceinline__ void product(const Pieces<float>& a, const Pieces<flo
   c = M::mul(a.s.hi, b.s.mid, c);
   c = M::mul(a.s.hi, b.s.hi, c);
 }
-template <typename M>
-__device__ __forceinline__ void product(const Pieces<uint16_t>& a, const Pieces<uint16_t>& b, bool two, typename M::Acc& c) {
-  if (two) c = M::mul(a.s.lo, b.s.hi, c);
+template <typename M, bool TWO>
+__device__ __forceinline__ void product(const Pieces<uint16_t>& a, const Pieces<uint16_t>& b, typename M::Acc& c) {
+  if (TWO) c = M::mul(a.s.lo, b.s.hi, c);
   c = M::mul(a.s.hi, b.s.hi, c);
 }
 
@@ -107,7 +107,9 @@ __device__ __forceinline__ void across(const T* __restrict__ p, int64_t ld, int6
 
 template <int T> constexpr int lds_floats() { return kWaves * T * T + kWaves * 64; }
 
-template <typename TI, typename TO, int FORM, bool VEC, int T>
+// TWO: dz in two pieces (beside bf16 operands).  LONG: K may have more than one run (a kernel of its own: the branch that is never
+// taken costs bf16 1024 x 256 x 256 backward 15.7 us instead of 13.4).
+template <typename TI, typename TO, int FORM, bool VEC, int T, bool LONG, bool TWO = false>
 __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t tn, float* lds) {
   using M = Mma<T>;
   constexpr int KC = 512 / T;  // k of a chunk
@@ -120,7 +122,7 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
   const TI* W = static_cast<const TI*>(g.W);
   const TO* gy = static_cast<const TO*>(g.grad_y);
   const TO* z = static_cast<const TO*>(g.preact_in);
-  const bool slope = g.act != SPCFG_ACT_NONE, two = FORM != FWD && dz_pieces<TI, TO>(g.act) == 2;
+  const bool slope = g.act != SPCFG_ACT_NONE;
 
   float* bl = lds + kWaves * T * T;  // [wave][64]
   // rows and columns past the end repeat the last one: their results are not stored
@@ -140,15 +142,15 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
 #pragma unroll
     for (int v = 0; v < M::V; ++v) {
       float* at = lds + wave * T * T + M::row(v, lane) * T + fr;
-      *at = run > kRun ? *at + acc[v] : acc[v];
+      *at = LONG && run > kRun ? *at + acc[v] : acc[v];
       acc[v] = 0.0f;
     }
-    if (FORM == DW) bl[wave * 64 + lane] = run > kRun ? bl[wave * 64 + lane] + bsum : bsum;
+    if (FORM == DW) bl[wave * 64 + lane] = LONG && run > kRun ? bl[wave * 64 + lane] + bsum : bsum;
     bsum = 0.0f;
     run += kRun;
   };
   for (int64_t c0 = wave; c0 < chunks; c0 += kWaves * U) {
-    if (c0 >= run) add_run();
+    if (LONG && c0 >= run) add_run();
     T1 va[U][8], vz[U][8];
     TI vb[U][8];
 #pragma unroll
@@ -187,10 +189,10 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
           times_slopes<8>(g.act, zz, d);
         }
         if (FORM == DW) bsum += ((d[0] + d[1]) + (d[2] + d[3])) + ((d[4] + d[5]) + (d[6] + d[7]));
-        A.dz(d, two);
+        A.template dz<TWO>(d);
       }
       B.raw(vb[u]);
-      product<M>(A, B, two, acc);
+      product<M, TWO>(A, B, acc);
     }
   }
 
@@ -220,20 +222,20 @@ __device__ __forceinline__ void tile_product(const Args& g, int64_t tm, int64_t 
   }
 }
 
-template <typename TI, typename TO, bool VEC, int T>
+template <typename TI, typename TO, bool VEC, int T, bool LONG>
 __global__ void __launch_bounds__(64 * kWaves) k_dense_forward(Args g, unsigned tiles_n, unsigned first) {
   __shared__ float lds[lds_floats<T>()];
   const unsigned b = first + blockIdx.x;
-  tile_product<TI, TO, FWD, VEC, T>(g, b / tiles_n, b % tiles_n, lds);
+  tile_product<TI, TO, FWD, VEC, T, LONG>(g, b / tiles_n, b % tiles_n, lds);
 }
 
 // both products of the backward pass in one launch: the tiles of dx first, then those of dW (either may be absent)
-template <typename TI, typename TO, bool VEC, int T>
+template <typename TI, typename TO, bool VEC, int T, bool LONG, bool TWO>
 __global__ void __launch_bounds__(64 * kWaves) k_dense_backward(Args g, unsigned tiles_x, unsigned tiles_i, unsigned first) {
   __shared__ float lds[lds_floats<T>()];
   const unsigned b = first + blockIdx.x;
-  if (b < tiles_x) tile_product<TI, TO, DX, VEC, T>(g, b / tiles_i, b % tiles_i, lds);
-  else tile_product<TI, TO, DW, VEC, T>(g, (b - tiles_x) / tiles_i, (b - tiles_x) % tiles_i, lds);
+  if (b < tiles_x) tile_product<TI, TO, DX, VEC, T, LONG, TWO>(g, b / tiles_i, b % tiles_i, lds);
+  else tile_product<TI, TO, DW, VEC, T, LONG, TWO>(g, (b - tiles_x) / tiles_i, (b - tiles_x) % tiles_i, lds);
 }
 
 unsigned tiles(int64_t n, int t) { return (unsigned)((n + t - 1) / t); }
@@ -248,34 +250,46 @@ void in_launches(unsigned n, F launch) {
   for (unsigned first = 0; first < n; first += kMostWorkgroups) launch(n - first < kMostWorkgroups ? n - first : kMostWorkgroups, first);
 }
 
-template <typename TI, typename TO, int T>
+template <typename TI, typename TO, int T, bool LONG>
 void forward(const Args& a, hipStream_t st) {
   const bool vec = on16(a.x) && on16(a.W) && a.I % 8 == 0;
   const unsigned tn = tiles(a.O, T);
   in_launches(tiles(a.R, T) * tn, [&](unsigned n, unsigned first) {
-    if (vec) hipLaunchKernelGGL((k_dense_forward<TI, TO, true, T>), dim3(n), dim3(64 * kWaves), 0, st, a, tn, first);
-    else hipLaunchKernelGGL((k_dense_forward<TI, TO, false, T>), dim3(n), dim3(64 * kWaves), 0, st, a, tn, first);
+    if (vec) hipLaunchKernelGGL((k_dense_forward<TI, TO, true, T, LONG>), dim3(n), dim3(64 * kWaves), 0, st, a, tn, first);
+    else hipLaunchKernelGGL((k_dense_forward<TI, TO, false, T, LONG>), dim3(n), dim3(64 * kWaves), 0, st, a, tn, first);
   });
 }
-template <typename TI, typename TO, int T>
+template <typename TI, typename TO, int T, bool LONG, bool TWO>
 void backward(const Args& a, hipStream_t st) {
   const bool vec = on16(a.grad_y) && on16(a.preact_in) && a.O % 8 == 0;
   const unsigned ti = tiles(a.I, T), tx = a.grad_x ? tiles(a.R, T) * ti : 0, tw = a.grad_W ? tiles(a.O, T) * ti : 0;
   in_launches(tx + tw, [&](unsigned n, unsigned first) {
-    if (vec) hipLaunchKernelGGL((k_dense_backward<TI, TO, true, T>), dim3(n), dim3(64 * kWaves), 0, st, a, tx, ti, first);
-    else hipLaunchKernelGGL((k_dense_backward<TI, TO, false, T>), dim3(n), dim3(64 * kWaves), 0, st, a, tx, ti, first);
+    if (vec) hipLaunchKernelGGL((k_dense_backward<TI, TO, true, T, LONG, TWO>), dim3(n), dim3(64 * kWaves), 0, st, a, tx, ti, first);
+    else hipLaunchKernelGGL((k_dense_backward<TI, TO, false, T, LONG, TWO>), dim3(n), dim3(64 * kWaves), 0, st, a, tx, ti, first);
   });
+}
+template <int T> bool is_long(int64_t K) { return K > (int64_t)kRun * (512 / T); }
+
+template <typename TI, typename TO, int T>
+void forward(const Args& a, hipStream_t st) {
+  if (is_long<T>(a.I)) forward<TI, TO, T, true>(a, st);
+  else forward<TI, TO, T, false>(a, st);
+}
+template <typename TI, typename TO, int T, bool TWO>
+void backward(const Args& a, hipStream_t st) {
+  if (is_long<T>(a.O > a.R ? a.O : a.R)) backward<TI, TO, T, true, TWO>(a, st);
+  else backward<TI, TO, T, false, TWO>(a, st);
 }
 template <typename TI, typename TO>
 void forward(const Args& a, hipStream_t st) {
   if (a.R <= 16 || tiles(a.R, 32) * tiles(a.O, 32) < kFew) forward<TI, TO, 16>(a, st);
   else forward<TI, TO, 32>(a, st);
 }
-template <typename TI, typename TO>
+template <typename TI, typename TO, bool TWO>
 void backward(const Args& a, hipStream_t st) {
   const unsigned ti = tiles(a.I, 32), n = (a.grad_x ? tiles(a.R, 32) * ti : 0) + (a.grad_W ? tiles(a.O, 32) * ti : 0);
-  if (n < kFew) backward<TI, TO, 16>(a, st);
-  else backward<TI, TO, 32>(a, st);
+  if (n < kFew) backward<TI, TO, 16, TWO>(a, st);
+  else backward<TI, TO, 32, TWO>(a, st);
 }
 
 }  // namespace
@@ -315,9 +329,10 @@ void launch_direct_forward(const Args& a, int in_type, int out_type, hipStream_t
   else forward<uint16_t, uint16_t>(a, st);
 }
 void launch_direct_backward(const Args& a, int in_type, int out_type, hipStream_t st) {
-  if (in_type == SPCFG_TYPE_F32) backward<float, float>(a, st);
-  else if (out_type == SPCFG_TYPE_F32) backward<uint16_t, float>(a, st);
-  else backward<uint16_t, uint16_t>(a, st);
+  if (in_type == SPCFG_TYPE_F32) backward<float, float, false>(a, st);
+  else if (out_type == SPCFG_TYPE_F32) backward<uint16_t, float, true>(a, st);
+  else if (dz_pieces<uint16_t, uint16_t>(a.act) == 2) backward<uint16_t, uint16_t, true>(a, st);
+  else backward<uint16_t, uint16_t, false>(a, st);
 }
 
 }  // namespace dense
