@@ -249,8 +249,7 @@ void launch_direct_backward(const Args& a, int in_type, int out_type, hipStream_
 
 // Tiled products (dense_tile.hip): workspace of a layer, 0 where it never takes them
 size_t tiled_workspace(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act);
-// whether these take the call: where they are estimated to be faster than products in registers, and what is read as it lies is on
-// 16 bytes
+// whether these take the call: where they are estimated to be faster than products in registers
 bool tiled_forward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
 bool tiled_backward(const Args& a, int in_type, int out_type, void* ws, hipStream_t st);
 

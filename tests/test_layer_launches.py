@@ -86,3 +86,12 @@ def test_long_sums_are_split(ask):
         for line, (rc, _, launches) in zip(lines, ask(lines)):
             names = [x[0] for x in launches]
             assert rc == 0 and "k_dense_backward_tiles" in names and "k_dense_backward_join" in names, (line, launches)
+
+
+def test_matrices_off_16_bytes_keep_to_tiles(ask):
+    """A large product of bf16 matrices takes tiles wherever they lie: what is off 16 bytes is laid out in the workspace first."""
+    for way in ("forward", "backward"):
+        for off in (2, 8):
+            line = f"{way} 8192 2048 2048 1 1 0 {off}"
+            (rc, _, launches), = ask([line])
+            assert rc == 0 and [x[0] for x in launches][:2] == ["k_dense_prepare", f"k_dense_{way}_tiles"], (line, launches)
