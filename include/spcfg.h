@@ -232,14 +232,16 @@ int spcfg_rules_backward(int32_t N, int32_t P, int32_t V, const float* log_root,
  *   x dev [rows x in], W dev [out x in], bias dev [out] or NULL, residual dev [rows x out] or NULL, y dev [rows x out]
  * x, W, bias and the gradients of all three have in_type; y, residual, preact and grad_y have out_type.  All matrices are
  * row-major and dense; their pointers need no more than the alignment of one element (16-byte alignment of rows is faster).
- *   in_type F32 (out_type F32): products of 16-bit pieces of the operands, accumulated in fp32, with the accuracy of an fp32
- *     product: three exact bf16 pieces of each value, or, in large forward products, two fp16 pieces of its row scaled by a
- *     power of two (values below 2^-29 of their row's largest are then good to 2^-51 of that one).  An infinite operand makes
- *     the results that it enters NaN, and one above 3.38e38 may.
+ *   in_type F32 (out_type F32): products of 16-bit pieces of the operands, accumulated in fp32: three exact bf16 pieces of each
+ *     value, each product x_k W_k good to 2^-23 of itself, or, in large forward products, two fp16 pieces of its row scaled by a
+ *     power of two, good to 2^-21 (values below 2^-29 of their row's largest are then good to 2^-51 of that one); the errors have
+ *     either sign, and those of long sums are no larger than an fp32 product's.  An infinite operand makes the results that it
+ *     enters NaN, and one above 3.38e38 may.
  *   in_type BF16 (out_type BF16 or F32): products of the given values accumulated in fp32.  The backward pass multiplies
  *     grad_y * act'(z), a value of fp32, as two bf16 pieces that hold it to 2^-17 (as one where it is a bf16 value); beside two
  *     pieces an infinite x or W makes the gradients that it enters NaN.
- * Activations and epilogues are computed in fp32 and rounded to the result's type once.
+ * Activations and epilogues are computed in fp32 and rounded to the result's type once.  GELU and SiLU are good to 2^-24 of
+ * themselves times 2.75 z^2 + 16 and 1.5 |z| + 8 where z < 0 (below 2^-126 |z| they may be 0), and to 2^-19 where z > 0.
  */
 enum { SPCFG_TYPE_F32 = 0, SPCFG_TYPE_BF16 = 1 };
 enum {
