@@ -244,7 +244,7 @@ inline bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 enum { FORWARD = 0, BACK_X = 1, BACK_W = 2, BACK = 3 };
 
 // Products in registers (dense_direct.hip), for any sizes, types and alignments; an estimate of what they take
-double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int what);
+double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int act, int what);
 void launch_direct_forward(const Args& a, int in_type, int out_type, hipStream_t st);
 void launch_direct_backward(const Args& a, int in_type, int out_type, hipStream_t st);
 

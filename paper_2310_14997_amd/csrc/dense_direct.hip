@@ -295,31 +295,37 @@ void backward(const Args& a, hipStream_t st) {
 }  // namespace
 
 // 3 us to start and end; then whichever is longer, the trips of one wavefront through k (counted in 128 values of a workgroup) or
-// those of all tiles on the whole chip, both fitted.  Measured (us for this kernel / on tiles in LDS): forward fp32 512^3 8.3 / 14,
-// 2048 x 512 x 512 22 / 18, 300 x 2000 x 300 16 / 24, 1000 x 701 x 900 25 / 22, bf16 5.5 / 6.9, 12 / 7.2, 9.0 / 18, 28 / 14;
-// backward fp32 512^3 20 / 19, 2000 x 30 x 30 15 / 22, 300 x 2000 x 300 40 / 25, bf16 12.2 / 11.6, 13 / 21, 26 / 13.
-double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int what) {
+// those of all tiles on the whole chip, both fitted on tiles of 16 and 32; backward more where the slope reads z.  Measured (us for
+// this kernel / on tiles in LDS): forward fp32 512^3 8.3 / 14, 2048 x 512 x 512 22 / 18, bf16 700^3 8.7 / 13, 8192 x 64 x 64 4.0 / 4.8,
+// 5108 x 355 x 355 30 / 14; backward fp32 512^3 18 / 19, 2048 x 128 x 128 32 / 18, 300 x 2000 x 300 27 / 22; bf16 to fp32
+// 4811 x 30 x 30 20 / 24, 512^3 9.6 / 12, 2048 x 128 x 128 17 / 14, 10 x 3692 x 3142 48 / 38.
+double direct_us(int64_t R, int64_t I, int64_t O, int in_type, int act, int what) {
   const bool fp32 = in_type == SPCFG_TYPE_F32;
   auto n = [](int64_t M, int64_t N) { return (double)tiles(M, 32) * tiles(N, 32); };
   auto trips = [](int64_t K) { return (double)((K + 127) / 128); };
   double longest = 0, all = 0, count = 0;
   if (what == FORWARD) {
     count = n(R, O);
-    longest = (fp32 ? 0.4 : 0.2) * trips(I);
-    all = (fp32 ? 0.0045 : I % 8 ? 0.0042 : 0.0021) * count * trips(I);
+    const bool small = R <= 16 || count < kFew;
+    longest = (fp32 ? (small ? 0.5 : 0.65) : small ? 0.25 : 0.68) * trips(I);
+    all = (fp32 ? (small ? 0.0048 : 0.0041) : (small ? 0.0018 : 0.0019) * (I % 8 ? 1.48 : 1)) * count * trips(I);
+  } else {
+    double work = 0, k = 0;
+    if (what & BACK_X) {
+      count += n(R, I);
+      work += n(R, I) * trips(O);
+      k = trips(O);
+    }
+    if (what & BACK_W) {
+      count += n(O, I);
+      work += n(O, I) * trips(R);
+      k = trips(R) > k ? trips(R) : k;
+    }
+    const bool small = count < kFew;
+    const double slope = act == SPCFG_ACT_NONE ? 1 : fp32 ? 1.58 : 1.42;
+    longest = (small ? 0.45 : fp32 ? 1.05 : 0.95) * k * slope;
+    all = (fp32 ? (small ? 0.0095 : 0.0046) : small ? 0.0055 : 0.003) * work * slope;
   }
-  if (what & BACK_X) {
-    count += n(R, I);
-    longest = (fp32 ? 0.75 : 0.65) * trips(O);
-    all += (fp32 ? 0.0085 : 0.0052) * n(R, I) * trips(O);
-  }
-  if (what & BACK_W) {
-    const double w = (fp32 ? 0.75 : 0.65) * trips(R);
-    count += n(O, I);
-    longest = longest > w ? longest : w;
-    all += (fp32 ? 0.0085 : 0.0052) * n(O, I) * trips(R);
-  }
-  if (count < kFew) all *= 1.6;  // (tiles of 16 read each operand twice as often)
   return 3 + (longest > all ? longest : all);
 }
 

@@ -802,14 +802,15 @@ Plan plan_of(int64_t R, int64_t I, int64_t O, int in_type, int out_type, int act
     consider(Tiling{128, 64, 512, 3, 5, 0.75, 0.67}, da, db, &p.c);
     consider(Tiling{256, 64, 256, 3, 15, 1.5, 1.75}, da, db, &p.c);
   }
-  // beside the products: a launch for planes and dz, 3 us and its bytes at 4 TB/s
+  // beside the products: a launch for planes and dz, 3 us (backward, with two kinds of workgroups in both launches, 5) and its bytes at
+  // 4 TB/s
   const double si = fp32 ? 4 : 2, so = out_type == SPCFG_TYPE_F32 ? 4 : 2;
   double bytes = 0;
   const double a_value = fp32 && what == FORWARD ? 8 : si * 2.5;
   if (p.cut) bytes += a_value * ((what != BACK_X ? (double)R * I : 0) + (what != BACK_W ? (double)O * I : 0));
   if (what != FORWARD) bytes += (double)R * O * ((act ? 2 : 1) * so + 2 * p.dz);
-  const double us = p.c.us + (bytes > 0 ? 3 + bytes / 4e6 : 0);
-  p.on = us < direct_us(R, I, O, in_type, what);
+  const double us = p.c.us + (what == FORWARD ? 0.5 : 2) + (bytes > 0 ? 3 + bytes / 4e6 : 0);
+  p.on = us < direct_us(R, I, O, in_type, act, what);
   if (!p.on) return p;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t o = at; at += (n + 255) / 256 * 256; return o; };
