@@ -25,8 +25,8 @@
 // No workgroup waits for another; sums run in an order fixed by the sizes.
 // Bound by the matrix cores on wide layers (bf16 8192^3 1250 TFLOP/s, 8192 x 4096 x 4096 with gelu 241 to 250 us = 1100 to 1140;
 // a library product of that size 1297), by LDS reads on tiles of 128 (700 to 800 TFLOP/s), by latency below some 2e9 products.
-// Backward 2048 x 512 x 10000 from fp32 gradients of bf16 layers: 132 us, of them two planes of dz 29, tiles 87 (two piece
-// products each, 970 TFLOP/s of them), joining parts 5.
+// Backward 2048 x 512 x 10000 from fp32 gradients of bf16 layers: 130 us, of them two planes of dz 29, tiles 88 (two piece
+// products each, 950 TFLOP/s of them), joining parts 5.
 #include <type_traits>
 #include <utility>
 
