@@ -146,8 +146,8 @@ struct Teacher {
   bool some, bad;       // whether any entry is there; whether an id is out of range or a score NaN or +inf
 };
 
-// Fills E with the row's ids and scores; an entry with a negative id or a score of -inf is absent, whatever else it holds.  This thread's share of the
-// largest score, and of whether something is wrong.
+// Fills E with the row's ids and scores; an entry with a negative id or a score of -inf is absent, whatever else it holds.  This
+// thread's share of the largest score, and of whether something is wrong.
 template <typename T, int NT>
 __device__ __forceinline__ void load_entries(const Args& g, int64_t row, Entries& E, float* top, float* wrong) {
   const T* t = static_cast<const T*>(g.teacher) + row * g.k;
